@@ -110,10 +110,9 @@ def draw(rng):
         if kind == "branch":
             share = rng.random() < 0.6
             parents, children = _log(rng, 1, 32), _log(rng, 1, 8)
-            tokens = parents * (lo + hi) / 2
-            copied = 0 if share else tokens * children
-            if tokens * hkv * d <= 2e8 and copied * hkv * d <= 1.2e8 and tokens * children <= 7e6:
-                return _branch(None, parents, children, lo, hi, hkv, d, budget, share, lens)
+            c = _branch(None, parents, children, lo, hi, hkv, d, budget, share, lens)
+            if parents * hi * hkv * d <= 2e8 and parents * hi * children <= 7e6 and work(c)["bytes"] <= 1.1e9:
+                return c
         else:
             reqs = _log(rng, 1, 128)
             tokens = 1 if rng.random() < 0.7 else rng.randrange(2, 64 // (hq // hkv) + 1)
