@@ -75,7 +75,7 @@ def listed():
         # a prompt scored token by token, the head's output padded
         _logprobs("logprobs_prompt", 4000, 151936, "bf16", 0, padded=64),
         # one conversation branched four ways, the branches dropped again: latency
-        _branch("branch_one", 1, 4, 2000, 2000, 8, 128),
+        _branch("branch_one", 1, 4, 2005, 2005, 8, 128),
         # a batch of traces branched eight ways: counts and tables of half a million pages
         _branch("branch_batch", 32, 8, 30000, 35000, 4, 128, lens=1006),
         # branches that own all their pages, as an in-place compaction needs: a copy
