@@ -9,7 +9,9 @@
  *     KVCache   <- Compaction(KVCache, KeepMask)             actkv_compact (fresh pages)
  *                                                            actkv_compact_inplace (Alg. 4)
  * and actkv_step / actkv_step_inplace run all three back to back on one stream;
- * actkv_lrfu_select / actkv_step_lrfu evict by LRFU keep scores (Sec. 5.1).
+ * actkv_lrfu_select / actkv_step_lrfu evict by LRFU keep scores (Sec. 5.1).  Between steps,
+ * actkv_attend runs decode attention on the cache, actkv_fork_pages and its fellows branch
+ * requests over shared pages, and actkv_token_confidence / actkv_token_logprobs read the logits.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -428,7 +430,6 @@ actkv_status actkv_budget_update(const float* token_conf, const int64_t* offsets
                                  int32_t* budgets_out, double* slopes, double* thresholds,
                                  int32_t* retained, void* stream);
 
-/* Static text for a status code. */
 /*
  * Device-side check of what the fresh-page compaction takes on trust (the caller's
  * guarantee to actkv_compact and actkv_step: the copies of Sec. 7.2 are conflict-free only
@@ -458,6 +459,121 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
                                const int32_t* free_pages, int64_t num_free, uint32_t* status,
                                void* scratch, size_t scratch_bytes, void* stream);
 
+/*
+ * Decode attention over the paged cache (Sec. 2.3, Sec. 2.5): for every action query j < n_r of
+ * request r -- here the request's newest tokens -- and query head g of KV head h,
+ *   out = sum_t p_t v_t,  p_t = exp(sm_scale q . k_t - LSE),  LSE = log sum_t exp(sm_scale q . k_t)
+ * over the entries t of (r, h) that it sees, and the LSE itself, which the scoring takes (Sec. 7.1:
+ * a by-product of decode attention).
+ *   kv_lens  device int32 [R * Hkv], or NULL for seq_lens[r] in every head: the entries of each
+ *            (request, KV head), the newest tokens included, as a compaction with unequal budgets
+ *            leaves them (new_lens, and n_r for the tokens appended since).  Read on the device, so
+ *            a captured call follows it; values outside [0, seq_lens[r]] are taken as the nearer
+ *            end, and seq_lens[r] is then only the most the block-table row holds.
+ *   causal   query j sees the entries t <= kv_lens - n_r + j (the newest tokens are the last n_r of
+ *            every head); otherwise all of them.
+ *   k_new, v_new  (both or neither) bf16 [sum n][Hkv][D], rows new_stride elements apart: the newest
+ *            tokens' K and V, which the call first writes to the entries kv_lens - n_r + j; those
+ *            below 0, and those whose page lies outside the pool, are not written.
+ *   q        bf16 [sum n][Hq][D], rows q_stride elements apart (Hq * D when it stands alone; the
+ *            parts of one fused projection have a larger stride).  Both strides: multiples of 8.
+ *   out      bf16 [sum n][Hq][D]; lse (nullable) fp32 [sum n][Hq], natural log.
+ * A query that sees no entry gets out = 0 and lse = -inf.  Slots past an entry count are never part
+ * of the result, whatever they hold.  Entries behind a page outside [0, num_pages) have K and V of
+ * zero (their logit is 0).  Sums and the softmax are fp32; the probabilities enter the second
+ * product as the sum of two bf16 values (16 bits).  At most 64 query rows per KV head and request
+ * (n_r * G), ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte aligned (lse and kv_lens: 4).  k_new,
+ * v_new, q, out and lse must not overlap the cache.  budgets are not used.  workspace: at least the
+ * bytes that actkv_attend_workspace reports (host only, callable without a device).  No atomics:
+ * results do not depend on scheduling.
+ */
+#define ACTKV_ATTEND_MAX_ROWS 64
+actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_bytes);
+actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_stride, void* kv_cache,
+                          const int32_t* block_table, const int32_t* kv_lens, const void* k_new,
+                          const void* v_new, int64_t new_stride, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Pages shared by several requests.  refs, int32 [num_pages] on the device, counts the requests
+ * that hold each page (0: free); it belongs to the caller and starts at zero.  A page held by more
+ * than one request must not be written: fresh-page compaction never does (acquire the fresh pages
+ * it took, release the pages it freed), the in-place compaction needs a request that owns its pages.
+ *
+ * actkv_acquire_pages: refs[page] += 1 for each of the n entries of pages.
+ * actkv_release_pages: refs[page] -= 1 for each of the n entries, never below 0; freed, int32 [n],
+ * receives the pages whose count came to 0, ascending, then -1; num_freed (device int32) their
+ * number.  A page that had no holder before is not listed.  workspace: at least the bytes that
+ * actkv_release_workspace reports (host only).
+ * Entries outside [0, num_pages) (the -1 of a block-table row's end) are passed over; a page may be
+ * listed several times.  pages and freed must not overlap.
+ */
+actkv_status actkv_acquire_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                                 void* stream);
+actkv_status actkv_release_workspace(int64_t n, int64_t num_pages, size_t* workspace_bytes);
+actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                                 int32_t* freed, int32_t* num_freed, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Forks of requests (the branches of an agent, parallel samples): fork f makes block-table row
+ * `child` a copy of row `parent` of `pages` pages, of which the first `shared` are shared and the
+ * others copied, K and V, into fresh ones:
+ *   child row [0, shared) = parent row [0, shared), and refs of each += 1;
+ *   child row [shared, pages) = fresh pages, free_pages[off .. off + pages - shared), off advancing
+ *     over the forks in order, whose refs become 1 and whose slots become the parent page's;
+ *   child row [pages, bt_stride) = -1.
+ * The pages that later appends of either may write are to be copied: with len_h entries in head h,
+ * shared = min_h len_h / page_size and pages = ceil(max_h len_h / page_size); shared = 0 gives the
+ * child pages of its own throughout.  Parent entries outside [0, num_pages) are taken over as they
+ * are where shared, and leave the fresh page unwritten where copied; fresh pages outside it are
+ * entered in the row and neither written nor counted.  refs may be NULL (nothing shared between
+ * live requests is counted).  forks_h: host array of num_forks, forks_d its device mirror.  Rows lie
+ * in [0, num_rows); a child is nobody's parent and the child of one fork only, and pages <=
+ * bt_stride.  free_pages must not contain live pages; fewer than needed: ACTKV_ERR_OUT_OF_PAGES.
+ * What a child's row held is overwritten (release it first).
+ */
+typedef struct actkv_fork {
+  int32_t parent, child, shared, pages;
+} actkv_fork;
+actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks_d,
+                              int32_t num_forks, int32_t num_rows, int32_t bt_stride,
+                              int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                              int64_t num_pages, void* kv_cache, int32_t* block_table,
+                              const int32_t* free_pages, int64_t num_free, int32_t* refs,
+                              void* stream);
+
+/*
+ * Log probabilities of given tokens, for a monitor or a client beside the token confidence.  For
+ * every row x of logits (the first `vocab` entries of rows row_stride elements apart, of element
+ * type logits_type; -inf entries are masked tokens):
+ *   logprobs[row] = x[tokens[row]] - LSE(x)  (0 where tokens[row] < 0, a row of padding; NaN where
+ *                   it is vocab or above); tokens: int64 [rows];
+ *   entropy[row]  = -sum_v p_v log p_v, p = softmax(x)  (a masked token adds nothing);
+ *   top_tokens[row][i], top_logprobs[row][i]  the i-th of the top_k largest entries, ties to the
+ *                   lower token (-0 equals +0), int64 and fp32; past a row of fewer than top_k
+ *                   entries: -1 and -inf.
+ * logprobs (with tokens), entropy, and the two top arrays (NULL together, or top_k 0) may each be
+ * NULL.  A row whose every token is masked has log probabilities of -inf and an entropy of 0.  Rows
+ * that hold +inf or NaN have unspecified values (never a fault; top_tokens stay within [-1, vocab)).
+ * Sums are fp32 per chunk of the row in a fixed order, joined in fp64: results do not depend on
+ * scheduling.  top_k in 0..64, vocab up to 262,144 (else ACTKV_ERR_UNSUPPORTED).  workspace: at
+ * least the bytes that actkv_token_logprobs_workspace reports.
+ */
+typedef enum actkv_logits_type {
+  ACTKV_LOGITS_F32 = 0,
+  ACTKV_LOGITS_BF16 = 1,
+  ACTKV_LOGITS_F16 = 2
+} actkv_logits_type;
+actkv_status actkv_token_logprobs_workspace(int64_t rows, int64_t vocab, int32_t top_k,
+                                            size_t* workspace_bytes);
+actkv_status actkv_token_logprobs(const void* logits, int32_t logits_type, int64_t rows,
+                                  int64_t vocab, int64_t row_stride, const int64_t* tokens,
+                                  int32_t top_k, float* logprobs, float* entropy,
+                                  int64_t* top_tokens, float* top_logprobs, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* Static text for a status code. */
 const char* actkv_status_str(actkv_status status);
 
 #ifdef __cplusplus

@@ -99,6 +99,20 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
               "actkv_token_confidence_workspace", "actkv_token_confidence",
               "actkv_budget_update"):
         getattr(lib, f).restype = ctypes.c_int
+    psz = ctypes.POINTER(sz)
+    lib.actkv_attend_workspace.argtypes = [P, psz]
+    lib.actkv_attend.argtypes = [P, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.actkv_acquire_pages.argtypes = [vp, i64, i64, vp, vp]
+    lib.actkv_release_workspace.argtypes = [i64, i64, psz]
+    lib.actkv_release_pages.argtypes = [vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.actkv_fork_pages.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i64, vp, vp, vp, i64, vp,
+                                     vp]
+    lib.actkv_token_logprobs_workspace.argtypes = [i64, i64, i32, psz]
+    lib.actkv_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    for f in ("actkv_attend_workspace", "actkv_attend", "actkv_acquire_pages",
+              "actkv_release_workspace", "actkv_release_pages", "actkv_fork_pages",
+              "actkv_token_logprobs_workspace", "actkv_token_logprobs"):
+        getattr(lib, f).restype = ctypes.c_int
     lib.actkv_check_pages.argtypes = [P, vp, vp, i64, vp, vp, sz, vp]
     lib.actkv_check_pages.restype = ctypes.c_int
     lib.actkv_set_overlap.argtypes = [i32]
@@ -116,12 +130,13 @@ class _Cache:
     reference to pass), the planning query, the sizes of every array, the pages the in-place
     compaction returns.  The struct holds the addresses of the host arrays `arrays`, which live as
     long as it does; `given` are the Problem's own, of which they may be copies."""
-    __slots__ = ("key", "given", "arrays", "struct", "ref", "query", "sizes", "inplace_freed")
+    __slots__ = ("key", "given", "arrays", "struct", "ref", "query", "sizes", "inplace_freed",
+                 "attend_ws")
 
     def __init__(self, key, given, arrays, struct):
         self.key, self.given, self.arrays = key, given, arrays
         self.struct, self.ref = struct, ctypes.byref(struct)
-        self.query = self.sizes = self.inplace_freed = None
+        self.query = self.sizes = self.inplace_freed = self.attend_ws = None
 
 
 @dataclass
@@ -811,6 +826,307 @@ def check_pages(p: Problem, block_table: torch.Tensor, free_pages: Optional[torc
         z.ref, _ptr(block_table), _ptr(free_pages), _numel(free_pages),
         _ptr(status), _ptr(scratch), _numel(scratch), _stream(stream)))
     return status
+
+
+class _Launch:
+    """Where a call's kernels go: the device of its tensors is made current around it, and the
+    stream is the caller's or that device's current one.  A buffer that the call makes for itself
+    (`scratch`) belongs to the stream it runs on, so that its memory is not handed out again while
+    the kernels run; one that the caller gets (`result`) is marked as in use there."""
+    __slots__ = ("device", "given", "handle", "_before")
+
+    def __init__(self, device: torch.device, stream):
+        self.device, self.given = device, stream
+
+    def __enter__(self):
+        self._before = torch._C._cuda_getDevice()
+        if self._before != self.device.index:
+            torch.cuda.set_device(self.device)
+        try:
+            self.handle = _stream(self.given)
+        except BaseException:
+            self.__exit__()
+            raise
+        return self
+
+    def __exit__(self, *exc):
+        if self._before != self.device.index:
+            torch.cuda.set_device(self._before)
+
+    def _torch_stream(self):
+        return (self.given if isinstance(self.given, torch.cuda.Stream)
+                else torch.cuda.ExternalStream(self.handle, device=self.device))
+
+    def scratch(self, size: int) -> torch.Tensor:
+        if self.given is None:
+            return torch.empty(max(size, 1), dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self._torch_stream()):
+            return torch.empty(max(size, 1), dtype=torch.uint8, device=self.device)
+
+    def result(self, shape, dtype) -> torch.Tensor:
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.given is not None and t.numel() > 0:
+            t.record_stream(self._torch_stream())
+        return t
+
+
+def _attend_ws(cache: _Cache) -> int:
+    if cache.attend_ws is None:
+        need = ctypes.c_size_t()
+        _check("actkv_attend_workspace",
+               load_library().actkv_attend_workspace(cache.ref, ctypes.byref(need)))
+        cache.attend_ws = need.value
+    return cache.attend_ws
+
+
+def attend_workspace(p: Problem, device="cuda") -> torch.Tensor:
+    """A workspace for attend() on p."""
+    return torch.empty(max(_attend_ws(p._cached()), 1), dtype=torch.uint8, device=device)
+
+
+def _token_rows(name: str, t, rows: int, heads: int, dim: int, seen: list) -> int:
+    """Checks [rows, heads, dim] bf16 whose rows may lie further apart than their elements (a part
+    of a fused projection); returns the distance in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if t.dtype not in _BITS16:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in _BITS16)}, got {t.dtype}")
+    if tuple(t.shape) != (rows, heads, dim):
+        raise ValueError(f"{name} must be [{rows}, {heads}, {dim}], got {list(t.shape)}")
+    seen.append((name, t))
+    if t.is_contiguous() or t.numel() == 0:
+        return heads * dim
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dim) or (rows > 1 and st[0] < heads * dim):
+        raise ValueError(f"{name}: the heads of a token must be contiguous, rows must not overlap")
+    return st[0] if rows > 1 else heads * dim
+
+
+def attend(p: Problem, q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor,
+           kv_lens: Optional[torch.Tensor] = None, k_new: Optional[torch.Tensor] = None,
+           v_new: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+           lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Decode attention of the requests' newest tokens (p.q_lens of them) over the paged cache.
+    q: [sum n, Hq, D]; kv_lens: int32 [R * Hkv] on the device, the entries of each (request, KV
+    head), or None for p.seq_lens; k_new, v_new: [sum n, Hkv, D], the newest tokens' K and V, written
+    to the cache first.  q, k_new and v_new may be parts of one fused projection (rows further
+    apart).  Returns (out [sum n, Hq, D], lse [sum n, Hq])."""
+    lib = load_library()
+    z = _Sizes(p)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    q_stride = _token_rows("q", q, z.sum_n, p.num_q_heads, p.head_dim, z.seen)
+    new_stride = 0
+    if k_new is not None:
+        new_stride = _token_rows("k_new", k_new, z.sum_n, p.num_kv_heads, p.head_dim, z.seen)
+        if _token_rows("v_new", v_new, z.sum_n, p.num_kv_heads, p.head_dim, z.seen) != new_stride:
+            raise ValueError("k_new and v_new must have the same distance between rows")
+    z.need("kv_cache", kv_cache, _BITS16, z.kv if z.scores else 0)
+    z.need("block_table", block_table, _I32, z.bt)
+    z.need("kv_lens", kv_lens, _I32, z.lens, required=False)
+    z.need("out", out, _BITS16, z.q, required=False)
+    z.need("lse", lse, _F32, z.lse, required=False)
+    need = _attend_ws(z.cache)
+    if ws is not None:
+        _need("ws", ws, None, 0, seen=z.seen)
+        if _ws_bytes(ws) < need:
+            raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
+    _on_gpu(z.seen + z.mirrors)
+    with _Launch(kv_cache.device, stream) as on:
+        if out is None:
+            out = on.result((z.sum_n, p.num_q_heads, p.head_dim), torch.bfloat16)
+        if lse is None:
+            lse = on.result((z.sum_n, p.num_q_heads), torch.float32)
+        ws = on.scratch(need) if ws is None else ws
+        _check("actkv_attend", lib.actkv_attend(
+            z.ref, _ptr(q), q_stride, _ptr(kv_cache), _ptr(block_table), _ptr(kv_lens), _ptr(k_new),
+            _ptr(v_new), new_stride, _ptr(out), _ptr(lse), _ptr(ws), _ws_bytes(ws), on.handle))
+    return out, lse
+
+
+@dataclass
+class Forks:
+    """Forks of requests for fork_pages: per fork the parent's and the child's block-table row, the
+    pages they share (the first ones) and the pages of the row; and their device mirror."""
+    parents: np.ndarray
+    children: np.ndarray
+    shared: np.ndarray
+    pages: np.ndarray
+    device: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        cols = [np.asarray(c, dtype=np.int32).reshape(-1)
+                for c in (self.parents, self.children, self.shared, self.pages)]
+        if len({c.shape[0] for c in cols}) != 1:
+            raise ValueError("parents, children, shared and pages must have the same length")
+        self.host = np.ascontiguousarray(np.stack(cols, axis=1))
+        self.host.setflags(write=False)   # the device mirror holds the same values
+        self.parents, self.children, self.shared, self.pages = self.host.T
+        self.num_fresh = int((self.pages.astype(np.int64) - self.shared).sum())
+
+    @classmethod
+    def of_lengths(cls, parents, children, kv_lens, share: bool = True) -> "Forks":
+        """kv_lens: entries of each (parent, KV head), [forks, Hkv] on the host.  Pages that are full
+        in every head are shared, the others copied (with share False all of them)."""
+        lens = np.asarray(kv_lens).reshape(len(np.asarray(parents).reshape(-1)), -1)
+        return cls(parents, children, lens.min(axis=1) // PAGE_SIZE * int(bool(share)),
+                   -(-lens.max(axis=1) // PAGE_SIZE))
+
+    def to_device(self, device="cuda") -> "Forks":
+        self.device = torch.from_numpy(self.host.copy()).to(device)
+        return self
+
+
+def fork_pages(forks: Forks, kv_cache: torch.Tensor, block_table: torch.Tensor,
+               free_pages: Optional[torch.Tensor], refs: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """Fills the children's rows of block_table [rows, stride]: shared pages counted in refs (int32
+    [num_pages]), the others copied into free_pages[: forks.num_fresh].  kv_cache: [2, pages, 16,
+    Hkv, D].  Returns block_table."""
+    lib = load_library()
+    seen: list = []
+    n = int(forks.host.shape[0])
+    if not isinstance(kv_cache, torch.Tensor) or kv_cache.dim() != 5 or kv_cache.shape[0] != 2:
+        raise ValueError("kv_cache must be [2, pages, page_size, kv heads, head dim]")
+    _, pages, page, heads, dim = (int(x) for x in kv_cache.shape)
+    _need("kv_cache", kv_cache, _BITS16, 0, seen=seen)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be [rows, stride]")
+    _need("block_table", block_table, _I32, 0, seen=seen)
+    _need("free_pages", free_pages, _I32, max(forks.num_fresh, 0), seen=seen)
+    _need("refs", refs, _I32, pages, required=False, seen=seen)
+    _need("forks", forks.device, _I32, 4 * n, seen=seen)
+    if refs is not None and refs.numel() != pages:
+        raise ValueError(f"refs holds {refs.numel()} counts, the cache {pages} pages")
+    _on_gpu(seen)
+    with _Launch(block_table.device, stream) as on:
+        _check("actkv_fork_pages", lib.actkv_fork_pages(
+            forks.host.ctypes.data, _ptr(forks.device), n, int(block_table.shape[0]),
+            int(block_table.shape[1]), heads, dim, page, pages, _ptr(kv_cache), _ptr(block_table),
+            _ptr(free_pages), _numel(free_pages), _ptr(refs), on.handle))
+    return block_table
+
+
+def acquire_pages(pages: torch.Tensor, refs: torch.Tensor, stream=None) -> torch.Tensor:
+    """refs[page] += 1 for every entry of pages (entries outside the pool are passed over)."""
+    lib = load_library()
+    seen: list = []
+    _need("pages", pages, _I32, 0, seen=seen)
+    _need("refs", refs, _I32, 1, seen=seen)
+    if pages is None:
+        raise ValueError("pages is required")
+    _on_gpu(seen)
+    with _Launch(refs.device, stream) as on:
+        _check("actkv_acquire_pages", lib.actkv_acquire_pages(
+            _ptr(pages), pages.numel(), refs.numel(), _ptr(refs), on.handle))
+    return refs
+
+
+_RELEASE_WS: dict = {}   # pool pages -> workspace bytes
+
+
+def _release_ws(num_pages: int) -> int:
+    if num_pages not in _RELEASE_WS:
+        need = ctypes.c_size_t()
+        _check("actkv_release_workspace",
+               load_library().actkv_release_workspace(0, num_pages, ctypes.byref(need)))
+        _RELEASE_WS[num_pages] = need.value
+    return _RELEASE_WS[num_pages]
+
+
+def release_workspace(num_pages: int, n: int, device="cuda") -> torch.Tensor:
+    """A workspace for release_pages() of n entries in a pool of num_pages."""
+    return torch.empty(max(_release_ws(int(num_pages)), 1), dtype=torch.uint8, device=device)
+
+
+def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch.Tensor] = None,
+                  num_freed: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                  stream=None):
+    """refs[page] -= 1 for every entry of pages; returns (freed, num_freed): the pages whose count
+    came to 0, ascending, then -1 (as many values as pages), and their number (int32 [1])."""
+    lib = load_library()
+    seen: list = []
+    if pages is None:
+        raise ValueError("pages is required")
+    _need("pages", pages, _I32, 0, seen=seen)
+    n = pages.numel()
+    _need("refs", refs, _I32, 1, seen=seen)
+    _need("freed", freed, _I32, n, required=False, seen=seen)
+    _need("num_freed", num_freed, _I32, 1, required=False, seen=seen)
+    need = _release_ws(refs.numel())
+    if ws is not None:
+        _need("ws", ws, None, 0, seen=seen)
+        if _ws_bytes(ws) < need:
+            raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
+    _on_gpu(seen)
+    with _Launch(refs.device, stream) as on:
+        if freed is None:
+            freed = on.result((n,), torch.int32)
+        if num_freed is None:
+            num_freed = on.result((1,), torch.int32)
+        ws = on.scratch(need) if ws is None else ws
+        _check("actkv_release_pages", lib.actkv_release_pages(
+            _ptr(pages), n, refs.numel(), _ptr(refs), _ptr(freed), _ptr(num_freed), _ptr(ws),
+            _ws_bytes(ws), on.handle))
+    return freed, num_freed
+
+
+_LOGITS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top_k: int = 0,
+                   logprobs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                   top_tokens: Optional[torch.Tensor] = None,
+                   top_logprobs: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                   stream=None) -> dict:
+    """Log probabilities of `tokens` (int64 [rows]; None: not wanted), the entropy and the top_k
+    largest entries of every row of `logits` (fp32, bf16 or fp16 [rows, vocab], unit column stride).
+    Returns logprobs, entropy, top_tokens and top_logprobs (None where not asked for)."""
+    lib = load_library()
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise ValueError("logits must be a 2-D tensor [rows, vocab]")
+    rows, vocab = int(logits.shape[0]), int(logits.shape[1])
+    if logits.dtype not in _LOGITS:
+        raise TypeError(f"logits must be float32, bfloat16 or float16, got {logits.dtype}")
+    if rows > 0 and vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("logits must have contiguous rows")
+    if rows > 1 and logits.stride(0) < vocab:
+        raise ValueError("logits rows must not overlap")
+    top_k = int(top_k)
+    seen = [("logits", logits)]
+    _need("tokens", tokens, (torch.int64,), rows, required=False, seen=seen)
+    if tokens is None and logprobs is not None:
+        raise ValueError("logprobs needs tokens")
+    _need("logprobs", logprobs, _F32, rows, required=False, seen=seen)
+    _need("entropy", entropy, _F32, rows, required=False, seen=seen)
+    _need("top_tokens", top_tokens, (torch.int64,), rows * top_k, required=False, seen=seen)
+    _need("top_logprobs", top_logprobs, _F32, rows * top_k, required=False, seen=seen)
+    need = ctypes.c_size_t()
+    _check("actkv_token_logprobs_workspace", lib.actkv_token_logprobs_workspace(
+        rows, vocab, top_k, ctypes.byref(need)))
+    if ws is not None:
+        _need("ws", ws, None, 0, seen=seen)
+        if _ws_bytes(ws) < need.value:
+            raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need.value}")
+    _on_gpu(seen)
+    with _Launch(logits.device, stream) as on:
+        if logprobs is None and tokens is not None:
+            logprobs = on.result((rows,), torch.float32)
+        if entropy is None:
+            entropy = on.result((rows,), torch.float32)
+        if top_k > 0:
+            if top_tokens is None:
+                top_tokens = on.result((rows, top_k), torch.int64)
+            if top_logprobs is None:
+                top_logprobs = on.result((rows, top_k), torch.float32)
+        else:
+            top_tokens = top_logprobs = None
+        ws = on.scratch(need.value) if ws is None else ws
+        _check("actkv_token_logprobs", lib.actkv_token_logprobs(
+            _ptr(logits), _LOGITS[logits.dtype], rows, vocab,
+            int(logits.stride(0)) if rows > 1 else vocab, _ptr(tokens), top_k, _ptr(logprobs),
+            _ptr(entropy), _ptr(top_tokens), _ptr(top_logprobs), _ptr(ws), _ws_bytes(ws), on.handle))
+    return dict(logprobs=logprobs, entropy=entropy, top_tokens=top_tokens, top_logprobs=top_logprobs)
 
 
 def set_overlap(groups: int) -> None:

@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libactkv.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "plan.hip", "score.hip", "select.hip", "compact.hip", "confidence.hip",
-           "noalloc.hip", "check.hip"]
+           "noalloc.hip", "check.hip", "attend.hip", "logprobs.hip", "pages.hip"]
 HEADERS = ["actkv_internal.h", "device_common.hpp", "lane_plan.hpp", "rewrite.hpp",
            "select_regs.hpp"]
 

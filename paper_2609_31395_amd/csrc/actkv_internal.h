@@ -280,4 +280,45 @@ hipError_t launch_compact_inplace(const DevProblem& dp, const HostPlan& hp, void
                                   int32_t* freed, int32_t* new_lens, int32_t* new_order,
                                   hipStream_t s);
 
+// Decode attention (actkv_attend).
+constexpr int kAttendUnit = 128;      // keys of a unit of work
+constexpr int kAttendMaxWgs = 1024;   // workgroups that share it
+struct AttendArgs {
+  int32_t R, Hq, Hkv, G, D, bt_stride, causal, max_rows;   // max_rows: most n * G of a request
+  int64_t num_pages, q_stride;
+  float alpha;                          // sm_scale * log2(e)
+  const int32_t *q_lens, *seq_lens, *kv_lens, *bt;
+  const uint16_t* q;
+  const char* kv;
+  uint16_t* out;
+  float* lse;
+  int32_t* seg_start;                   // workspace [R * Hkv + 1]: units before each segment
+  int32_t* q_off;                       // workspace [R]
+  float* part_o;                        // workspace [2 * workgroups][max_rows][D]
+  float2* part_ml;                      // workspace [2 * workgroups][max_rows]: shift and sum
+};
+hipError_t launch_append(const AttendArgs& a, int64_t max_n, const void* k_new, const void* v_new,
+                         int64_t stride, hipStream_t s);
+// units: the most there can be (from the host's lengths)
+hipError_t launch_attend(const AttendArgs& a, int64_t units, hipStream_t s);
+
+// Shared pages (actkv_acquire_pages and its fellows).
+constexpr int64_t kReleaseBlock = 8192;   // pages whose freed ones one workgroup lists
+inline int64_t release_blocks(int64_t num_pages) { return (num_pages + kReleaseBlock - 1) / kReleaseBlock; }
+hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t max_copied, int32_t bt_stride,
+                       int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
+                       const int32_t* free_pages, int32_t* refs, hipStream_t s);
+hipError_t launch_acquire(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                          hipStream_t s);
+// words: of the bitmap and the blocks' counts behind it, cleared first
+hipError_t launch_release(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                          int32_t* freed, int32_t* num_freed, uint32_t* bits, uint32_t* counts,
+                          int64_t words, hipStream_t s);
+// Token log probabilities: chunks of kConfChunkLogits logits, conf_splits(vocab) to a row; stats holds
+// 3 floats and top k keys per chunk.
+hipError_t launch_token_logprobs(const void* logits, int type, int64_t rows, int64_t vocab,
+                                 int64_t row_stride, const int64_t* tokens, int k, float* logprobs,
+                                 float* entropy, int64_t* top_tokens, float* top_logprobs,
+                                 float* stats, unsigned long long* top, hipStream_t s);
+
 }  // namespace actkv

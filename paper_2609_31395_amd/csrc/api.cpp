@@ -5,6 +5,7 @@
 
 #include <atomic>
 #include <mutex>
+#include <new>
 #include <vector>
 
 #include "actkv.h"
@@ -895,6 +896,232 @@ actkv_status actkv_budget_update(const float* token_conf, const int64_t* offsets
   return hip_status(actkv::launch_budget_update(
       token_conf, offsets_d, num_reqs, window, stride, bottom_pct, scale_up, budget_upper,
       budgets_in, budgets_out, slopes, thresholds, retained, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Decode attention: the problem's rows and units, and where its workspace lies.
+struct AttendPlan {
+  HostPlan hp;
+  int64_t units = 0, max_rows = 0;
+  size_t seg_start = 0, q_off = 0, part_ml = 0, part_o = 0, total = 0;
+};
+
+actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
+  const actkv_status st = plan_host(p, &ap->hp);
+  if (st != ACTKV_OK) return st;
+  const HostPlan& hp = ap->hp;
+  ap->max_rows = hp.max_n * hp.G;
+  if (ap->max_rows > ACTKV_ATTEND_MAX_ROWS) return ACTKV_ERR_UNSUPPORTED;
+  for (int r = 0; r < hp.R; ++r)
+    ap->units += (p->seq_lens_h[r] + (int64_t)actkv::kAttendUnit - 1) / actkv::kAttendUnit * hp.Hkv;
+  const int64_t segs = (int64_t)hp.R * hp.Hkv;
+  if (ap->units > INT32_MAX / 2 || segs > INT32_MAX / 2) return ACTKV_ERR_UNSUPPORTED;
+  const int64_t slots = 2 * (ap->units < actkv::kAttendMaxWgs ? ap->units : actkv::kAttendMaxWgs);
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = actkv::align256(o + bytes); return at; };
+  ap->seg_start = take(sizeof(int32_t) * (size_t)(segs + 1));
+  ap->q_off = take(sizeof(int32_t) * (size_t)hp.R);
+  ap->part_ml = take(2 * sizeof(float) * (size_t)(slots * ap->max_rows));
+  ap->part_o = take(sizeof(float) * (size_t)(slots * ap->max_rows * hp.D));
+  ap->total = o;
+  return ACTKV_OK;
+}
+
+}  // namespace
+
+actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_bytes) {
+  AttendPlan ap;
+  const actkv_status st = plan_attend(p, &ap);
+  if (st != ACTKV_OK) return st;
+  if (workspace_bytes) *workspace_bytes = ap.total;
+  return ACTKV_OK;
+}
+
+actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_stride, void* kv_cache,
+                          const int32_t* block_table, const int32_t* kv_lens, const void* k_new,
+                          const void* v_new, int64_t new_stride, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  AttendPlan ap;
+  actkv_status st = plan_attend(p, &ap);
+  if (st != ACTKV_OK) return st;
+  const HostPlan& hp = ap.hp;
+  if (hp.R > 0 && (!p->seq_lens_d || !p->q_lens_d)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if ((k_new == nullptr) != (v_new == nullptr)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (q_stride < (int64_t)hp.Hq * hp.D || q_stride % 8) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (k_new && (new_stride < (int64_t)hp.Hkv * hp.D || new_stride % 8)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (!aligned16(q) || !aligned16(kv_cache) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) ||
+      !aligned16(workspace))
+    return ACTKV_ERR_INVALID_ARGUMENT;
+  if (hp.sum_n > 0 && (!q || !out)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (hp.sum_n > 0 && hp.sum_L > 0 && (!kv_cache || !block_table)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < ap.total) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
+  if (!workspace) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (hp.sum_n == 0) return ACTKV_OK;
+  char* base = static_cast<char*>(workspace);
+  actkv::AttendArgs a = {};
+  a.R = hp.R;
+  a.Hq = hp.Hq;
+  a.Hkv = hp.Hkv;
+  a.G = hp.G;
+  a.D = hp.D;
+  a.bt_stride = p->bt_stride;
+  a.causal = p->causal;
+  a.max_rows = (int32_t)ap.max_rows;
+  a.num_pages = p->num_pages;
+  a.q_stride = q_stride;
+  a.alpha = (p->sm_scale > 0.f ? p->sm_scale : 1.0f / sqrtf((float)p->head_dim)) * 1.4426950408889634f;
+  a.q_lens = p->q_lens_d;
+  a.seq_lens = p->seq_lens_d;
+  a.kv_lens = kv_lens;
+  a.bt = block_table;
+  a.q = static_cast<const uint16_t*>(q);
+  a.kv = static_cast<const char*>(kv_cache);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.seg_start = reinterpret_cast<int32_t*>(base + ap.seg_start);
+  a.q_off = reinterpret_cast<int32_t*>(base + ap.q_off);
+  a.part_ml = reinterpret_cast<float2*>(base + ap.part_ml);
+  a.part_o = reinterpret_cast<float*>(base + ap.part_o);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (k_new && hp.sum_L > 0) {
+    st = hip_status(actkv::launch_append(a, hp.max_n, k_new, v_new, new_stride, s));
+    if (st != ACTKV_OK) return st;
+  }
+  return hip_status(actkv::launch_attend(a, ap.units, s));
+}
+
+actkv_status actkv_acquire_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                                 void* stream) {
+  if (n < 0 || num_pages <= 0) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (n == 0) return ACTKV_OK;
+  if (!pages || !refs) return ACTKV_ERR_INVALID_ARGUMENT;
+  return hip_status(actkv::launch_acquire(pages, n, num_pages, refs, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+actkv_status check_release(int64_t n, int64_t num_pages) {
+  if (n < 0 || num_pages <= 0) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (num_pages > INT32_MAX) return ACTKV_ERR_UNSUPPORTED;   // page ids are int32
+  return ACTKV_OK;
+}
+int64_t release_words(int64_t num_pages) {
+  return (num_pages + 31) / 32 + actkv::release_blocks(num_pages);
+}
+}  // namespace
+
+actkv_status actkv_release_workspace(int64_t n, int64_t num_pages, size_t* workspace_bytes) {
+  const actkv_status st = check_release(n, num_pages);
+  if (st != ACTKV_OK) return st;
+  if (workspace_bytes) *workspace_bytes = sizeof(uint32_t) * (size_t)release_words(num_pages);
+  return ACTKV_OK;
+}
+
+actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
+                                 int32_t* freed, int32_t* num_freed, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const actkv_status st = check_release(n, num_pages);
+  if (st != ACTKV_OK) return st;
+  if (!num_freed || (n > 0 && (!pages || !refs || !freed)) || (pages && pages == freed))
+    return ACTKV_ERR_INVALID_ARGUMENT;
+  const int64_t words = release_words(num_pages);
+  if (workspace_bytes < sizeof(uint32_t) * (size_t)words) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3)) return ACTKV_ERR_INVALID_ARGUMENT;
+  uint32_t* bits = static_cast<uint32_t*>(workspace);
+  return hip_status(actkv::launch_release(pages, n, num_pages, refs, freed, num_freed, bits,
+                                          bits + (num_pages + 31) / 32, words,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks_d,
+                              int32_t num_forks, int32_t num_rows, int32_t bt_stride,
+                              int32_t num_kv_heads, int32_t head_dim, int32_t page_size,
+                              int64_t num_pages, void* kv_cache, int32_t* block_table,
+                              const int32_t* free_pages, int64_t num_free, int32_t* refs,
+                              void* stream) {
+  if (num_forks < 0 || num_rows < 0 || bt_stride <= 0 || num_kv_heads <= 0 || head_dim <= 0 ||
+      page_size <= 0 || num_pages <= 0 || num_free < 0)
+    return ACTKV_ERR_INVALID_ARGUMENT;
+  if ((head_dim != 64 && head_dim != 128) || page_size != actkv::kPageSize || num_kv_heads > 64 ||
+      num_forks > 65535)
+    return ACTKV_ERR_UNSUPPORTED;
+  if (num_forks == 0) return ACTKV_OK;
+  if (!forks_h || !forks_d || !block_table) return ACTKV_ERR_INVALID_ARGUMENT;
+  int64_t fresh = 0, most = 0;
+  try {
+    std::vector<uint8_t> row(num_rows, 0);   // 1: a parent, 2: a child
+    for (int f = 0; f < num_forks; ++f) {
+      const actkv_fork& k = forks_h[f];
+      if (k.parent < 0 || k.parent >= num_rows || k.child < 0 || k.child >= num_rows || k.shared < 0 ||
+          k.pages < k.shared || k.pages > bt_stride)
+        return ACTKV_ERR_INVALID_ARGUMENT;
+      if (row[k.parent] == 2 || row[k.child] != 0 || k.parent == k.child) return ACTKV_ERR_INVALID_ARGUMENT;
+      row[k.parent] = 1;
+      row[k.child] = 2;
+      fresh += k.pages - k.shared;
+      most = k.pages - k.shared > most ? k.pages - k.shared : most;
+    }
+  } catch (const std::bad_alloc&) {
+    return ACTKV_ERR_HIP;
+  }
+  if (fresh > 0 && (!kv_cache || !aligned16(kv_cache))) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (num_free < fresh) return ACTKV_ERR_OUT_OF_PAGES;
+  if (fresh > 0 && !free_pages) return ACTKV_ERR_INVALID_ARGUMENT;
+  return hip_status(actkv::launch_fork(
+      forks_d, num_forks, most, bt_stride, num_pages,
+      (int64_t)page_size * num_kv_heads * head_dim * 2, kv_cache, block_table, free_pages, refs,
+      static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+actkv_status check_logprobs(int64_t rows, int64_t vocab, int32_t top_k) {
+  if (rows < 0 || vocab < 1 || top_k < 0) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (top_k > actkv::kConfMaxTopK) return ACTKV_ERR_UNSUPPORTED;
+  if (vocab > (int64_t)actkv::kConfMaxSplits * actkv::kConfChunkLogits) return ACTKV_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX / actkv::kConfMaxSplits) return ACTKV_ERR_UNSUPPORTED;
+  return ACTKV_OK;
+}
+size_t logprobs_stats(int64_t rows, int64_t vocab) {
+  return actkv::align256(3 * sizeof(float) * (size_t)(rows * actkv::conf_splits(vocab)));
+}
+}  // namespace
+
+actkv_status actkv_token_logprobs_workspace(int64_t rows, int64_t vocab, int32_t top_k,
+                                            size_t* workspace_bytes) {
+  const actkv_status st = check_logprobs(rows, vocab, top_k);
+  if (st != ACTKV_OK) return st;
+  if (workspace_bytes)
+    *workspace_bytes = logprobs_stats(rows, vocab) +
+                       sizeof(uint64_t) * (size_t)(rows * actkv::conf_splits(vocab) * top_k);
+  return ACTKV_OK;
+}
+
+actkv_status actkv_token_logprobs(const void* logits, int32_t logits_type, int64_t rows,
+                                  int64_t vocab, int64_t row_stride, const int64_t* tokens,
+                                  int32_t top_k, float* logprobs, float* entropy,
+                                  int64_t* top_tokens, float* top_logprobs, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  if (!top_tokens && !top_logprobs) top_k = 0;
+  size_t need = 0;
+  const actkv_status st = actkv_token_logprobs_workspace(rows, vocab, top_k, &need);
+  if (st != ACTKV_OK) return st;
+  if (logits_type < ACTKV_LOGITS_F32 || logits_type > ACTKV_LOGITS_F16 || row_stride < vocab)
+    return ACTKV_ERR_INVALID_ARGUMENT;
+  if (rows == 0) return ACTKV_OK;
+  const uintptr_t size = logits_type == ACTKV_LOGITS_F32 ? 4 : 2;
+  if (!logits || reinterpret_cast<uintptr_t>(logits) % size) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (logprobs && !tokens) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (top_k > 0 && (!top_tokens || !top_logprobs)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < need) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7)) return ACTKV_ERR_INVALID_ARGUMENT;
+  char* base = static_cast<char*>(workspace);
+  return hip_status(actkv::launch_token_logprobs(
+      logits, logits_type, rows, vocab, row_stride, tokens, top_k, logprobs, entropy, top_tokens,
+      top_logprobs, reinterpret_cast<float*>(base),
+      reinterpret_cast<unsigned long long*>(base + logprobs_stats(rows, vocab)),
+      static_cast<hipStream_t>(stream)));
 }
 
 const char* actkv_status_str(actkv_status status) {
