@@ -10,6 +10,8 @@
 // The mathematics of a piece, per query row: a shift m, l = sum 2^(x_t - m) and o = sum 2^(x_t - m) v_t
 // over its entries, x_t = sm_scale log2(e) q.k_t.  Two pieces join as m = max(m1, m2),
 // l = l1 2^(m1 - m) + l2 2^(m2 - m) and the same for o; out = o / l, LSE = (m + log2 l) ln 2.
+#include <type_traits>
+
 #include "device_common.hpp"
 
 namespace actkv {
@@ -42,19 +44,40 @@ __device__ __forceinline__ int units_of(const Segment& g) {
   return g.n > 0 ? ceil_div(g.len, kUnit) : 0;
 }
 
-// The largest w with floor(total * w / wgs) <= u: the workgroup that holds unit u.
-__device__ __forceinline__ int workgroup_of(int64_t u, int64_t total, int64_t wgs) {
-  return (int)(((u + 1) * wgs + total - 1) / total) - 1;
-}
+// Equal shares of `total` units for at most `grid` workgroups, the first `more` of them a unit larger
+// (no more workgroups than units: each of them holds one at least).
+struct Shares {
+  int wgs, each, more;
+  __device__ __forceinline__ Shares(int total, int grid) {
+    wgs = min(total, grid);
+    each = wgs > 0 ? total / wgs : 1;
+    more = total - wgs * each;
+  }
+  __device__ __forceinline__ int begin(int b) const { return b * each + min(b, more); }
+  __device__ __forceinline__ int holder(int unit) const {   // the workgroup whose share it is in
+    const int large = more * (each + 1);
+    return unit < large ? unit / (each + 1) : more + (unit - large) / each;
+  }
+};
 
 __device__ __forceinline__ float xor_max(float v, int d) { return fmaxf(v, __shfl_xor(v, d, 64)); }
 __device__ __forceinline__ float xor_sum(float v, int d) { return v + __shfl_xor(v, d, 64); }
+
+// Steps of K and V a wave has in flight, and workgroups per CU (a wave of each on every SIMD), by what
+// fits the registers.
+template <int D, int kRowTiles>
+struct Shape {
+  static constexpr int kRing = (D == 128 ? kRowTiles == 1 : kRowTiles <= 2) ? 2 : 1;
+  static constexpr int kWgs = D == 128 ? (kRowTiles <= 2 ? 2 : 1) : (kRowTiles == 1 ? 3 : 2);
+};
 
 // Operands of one step (32 keys of two pages), as loaded: lane l = 16 c + i holds, of K, 16 bytes
 // of entry i of either page per 32 elements, and of V the 16th i of entries 4 c .. 4 c + 3 of either
 // page.  The first is the A operand of S^T = K Q^T; its result leaves lane l with the logits of query
 // row i for exactly the entries 4 c .. 4 c + 3 of either page, which is the B operand of
 // O^T = V^T P^T for V in this order: the probabilities never change lanes.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 template <int D>
 struct Operands {
   static constexpr int kSteps = D / 32;         // MFMAs of a product over the head dimension
@@ -86,14 +109,14 @@ struct Rows {
 }  // namespace
 
 template <int D, int kRowTiles>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, (Shape<D, kRowTiles>::kWgs)) void attend_kernel(AttendArgs a) {
   using Op = Operands<D>;
-  constexpr int kE = D / 16, kRing = kRowTiles == 4 ? 1 : 2;
+  constexpr int kE = D / 16, kRing = Shape<D, kRowTiles>::kRing;
   constexpr int kOStride = D + 4;
   __shared__ __align__(16) float o_s[kWaves][16][kOStride];
   __shared__ float m_s[kWaves][16], l_s[kWaves][16];
   __shared__ int64_t scan_s[17];
-  __shared__ int first_s[3];
+  __shared__ int first_s[5];
   const int tid = threadIdx.x, lane = tid & 63, c = lane >> 4, i16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int S = a.R * a.Hkv, b = blockIdx.x;
@@ -101,55 +124,57 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
   // the plan: units and new tokens before each segment (every workgroup finds its own share)
   const int per = ceil_div(S, kThreads);
   int64_t own = 0;
-  for (int s = tid * per; s < S && s < (tid + 1) * per; ++s) {
-    const Segment g = segment(a, s);
-    own += ((int64_t)units_of(g) << 32) + (s % a.Hkv == 0 ? g.n : 0);
+  Segment g = {0, 0};   // this thread's (last) segment
+  for (int x = tid * per; x < S && x < (tid + 1) * per; ++x) {
+    g = segment(a, x);
+    own += ((int64_t)units_of(g) << 32) + (x % a.Hkv == 0 ? g.n : 0);
   }
   int64_t all;
   const int64_t before = block_excl_scan_i64(own, scan_s, &all);
-  const int64_t total = all >> 32;
-  // (no more workgroups than units: each of them then holds a unit at least)
-  const int64_t wgs = total < (int64_t)gridDim.x ? total : (int64_t)gridDim.x;
-  const int64_t c0 = b < wgs ? total * b / wgs : 0, c1 = b < wgs ? total * (b + 1) / wgs : 0;
-  const int64_t u_before = before >> 32;
-  const bool mine = c0 < c1 && u_before <= c0 && c0 < u_before + (own >> 32);
+  const int total = (int)(all >> 32);
+  const Shares shares(total, gridDim.x);
+  const int c0 = b < shares.wgs ? shares.begin(b) : 0, c1 = b < shares.wgs ? shares.begin(b + 1) : 0;
+  const int u_before = (int)(before >> 32);
+  const bool mine = c0 < c1 && u_before <= c0 && c0 < u_before + (int)(own >> 32);
   if (mine || b == 0) {
-    int64_t u = u_before, q = before & 0xFFFFFFFF;
-    for (int s = tid * per; s < S && s < (tid + 1) * per; ++s) {
-      const Segment g = segment(a, s);
-      const int h = s % a.Hkv, n_units = units_of(g);
+    int u = u_before, q = (int)before;
+    for (int x = tid * per; x < S && x < (tid + 1) * per; ++x) {
+      if (per > 1) g = segment(a, x);
+      const int h = x % a.Hkv, n_units = units_of(g);
       if (b == 0) {
-        a.seg_start[s] = (int32_t)u;
-        if (h == 0) a.q_off[s / a.Hkv] = (int32_t)q;
+        a.seg_start[x] = u;
+        if (h == 0) a.q_off[x / a.Hkv] = q;
       }
       if (mine && u <= c0 && c0 < u + n_units) {
-        first_s[0] = s;
-        first_s[1] = (int)u;
-        first_s[2] = (int)(h == 0 ? q : q - g.n);
+        first_s[0] = x;
+        first_s[1] = u;
+        first_s[2] = h == 0 ? q : q - g.n;
+        first_s[3] = g.len;
+        first_s[4] = g.n;
       }
       u += n_units;
       if (h == 0) q += g.n;
     }
-    if (b == 0 && tid == 0) a.seg_start[S] = (int32_t)total;
+    if (b == 0 && tid == 0) a.seg_start[S] = total;
   }
   if (c0 >= c1) return;
   __syncthreads();
   int s = __builtin_amdgcn_readfirstlane(first_s[0]);
-  int64_t start = __builtin_amdgcn_readfirstlane(first_s[1]);
+  int start = __builtin_amdgcn_readfirstlane(first_s[1]);
   int q_off = __builtin_amdgcn_readfirstlane(first_s[2]);
+  int len = __builtin_amdgcn_readfirstlane(first_s[3]);
+  int n = __builtin_amdgcn_readfirstlane(first_s[4]);
 
   const int64_t page_bytes = (int64_t)kPageSize * a.Hkv * D * 2;
   const int64_t v_plane = a.num_pages * page_bytes;
   const int row_bytes = a.Hkv * D * 2;
+  const int32_t num_pages32 = (int32_t)(a.num_pages < INT32_MAX ? a.num_pages : INT32_MAX);
 
-  for (; s < S && start < c1; ++s) {
-    const Segment g = segment(a, s);
+  for (;;) {
     const int r = s / a.Hkv, h = s % a.Hkv;
-    const int len = __builtin_amdgcn_readfirstlane(g.len), n = __builtin_amdgcn_readfirstlane(g.n);
     const int n_units = n > 0 ? ceil_div(len, kUnit) : 0;
     if (n_units > 0) {
-      const int u0 = (int)(c0 > start ? c0 - start : 0);
-      const int u1 = (int)(c1 - start < n_units ? c1 - start : n_units);
+      const int u0 = max(c0 - start, 0), u1 = min(c1 - start, n_units);
       const bool whole = u0 == 0 && u1 == n_units;
       const int rows = n * a.G;
       const int keys_end = min(u1 * kUnit, len);
@@ -174,63 +199,63 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
       const int all_see = a.causal ? len - n + 1 : len;   // entries below it are seen by every row
 
       const int32_t* bt_row = a.bt + (int64_t)r * a.bt_stride;
-      const char* k_lane = a.kv + (int64_t)i16 * row_bytes + h * D * 2 + 16 * c;
-      const char* v_lane = a.kv + v_plane + (int64_t)4 * c * row_bytes + h * D * 2 + 2 * kE * i16;
+      const char* k_head = a.kv + h * D * 2;
+      const uint32_t k_off = (uint32_t)(i16 * row_bytes + 16 * c);
+      uint32_t v_off[4];   // (in the lane's offset: the bounds check takes a scalar one off the size)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) v_off[y] = (uint32_t)((4 * c + y) * row_bytes + 2 * kE * i16);
       Op ring[kRing];
-      bool bad[kRing][2];
+      // this wave's steps: u0 * kWaves + w, and every kWaves-th from there
       const int i_first = u0 * kWaves + w;
-      // this wave's last step (i_first - kWaves: none)
-      const int steps_end = ceil_div(keys_end, kStep);
-      const int i_last = steps_end > i_first
-                             ? i_first + (steps_end - 1 - i_first) / kWaves * kWaves : i_first - kWaves;
-      auto issue = [&](int slot, int i) {
+      const int steps = max(ceil_div(ceil_div(keys_end, kStep) - i_first, kWaves), 0);
+      // Their pages, 32 steps at a time: lane l holds the id of page l % 2 of step l / 2 and how many
+      // bytes of it, from this head's first row on, hold entries.  Loads past those bytes read as
+      // zero and move nothing: the slots behind the entries (which may hold anything, and 0 times a
+      // NaN of theirs would be one), pages outside the pool, and steps past the wave's last, which
+      // are issued like the others so that every wait counts the same loads.
+      int32_t page_next = 0, page_now = 0, bytes_now = 0;
+      auto fetch_pages = [&](int x) {
+        page_next = bt_row[min(2 * (i_first + (x + (lane >> 1)) * kWaves) + (lane & 1), pages - 1)];
+      };
+      auto take_pages = [&](int x) {
+        const int step = x + (lane >> 1);
+        const int held = min(len - kPageSize * (2 * (i_first + step * kWaves) + (lane & 1)), kPageSize);
+        const bool ok = step < steps && held > 0 && page_next >= 0 && page_next < num_pages32;
+        page_now = ok ? page_next : 0;
+        bytes_now = ok ? (held - 1) * row_bytes + 2 * D : 0;
+      };
+      auto issue = [&](int slot, int x) {   // step x of the wave
+        if ((x & 31) == 0) {
+          take_pages(x);
+          fetch_pages(x + 32);
+        }
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
-          const int p = min(2 * i + sub, pages - 1);
-          int64_t page = bt_row[p];
-          bad[slot][sub] = page < 0 || page >= a.num_pages;
-          if (bad[slot][sub]) page = 0;   // never dereference outside the pool
-          const char* kp = k_lane + page * page_bytes;
-          const char* vp = v_lane + page * page_bytes;
+          const int64_t page = __builtin_amdgcn_readlane(page_now, 2 * (x & 31) + sub);
+          const int bytes = __builtin_amdgcn_readlane(bytes_now, 2 * (x & 31) + sub);
+          const char* kp = k_head + page * page_bytes;
+          const __amdgpu_buffer_rsrc_t kr = buffer_over(kp, bytes), vr = buffer_over(kp + v_plane, bytes);
 #pragma unroll
           for (int ks = 0; ks < Op::kSteps; ++ks)
-            ring[slot].k[sub][ks] = *reinterpret_cast<const u32x4*>(kp + 64 * ks);
+            ring[slot].k[sub][ks] = __builtin_amdgcn_raw_buffer_load_b128(kr, k_off + 64 * ks, 0, 0);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
+          for (int y = 0; y < 4; ++y) {
             if constexpr (D == 128) {
-              const u32x4 t = *reinterpret_cast<const u32x4*>(vp + x * row_bytes);
+              const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(vr, v_off[y], 0, 0);
 #pragma unroll
-              for (int y = 0; y < 4; ++y) ring[slot].v[4 * sub + x][y] = t[y];
+              for (int z = 0; z < 4; ++z) ring[slot].v[4 * sub + y][z] = t[z];
             } else {
-              const uint2 t = *reinterpret_cast<const uint2*>(vp + x * row_bytes);
-              ring[slot].v[4 * sub + x][0] = t.x;
-              ring[slot].v[4 * sub + x][1] = t.y;
+              const u32x2 t = __builtin_amdgcn_raw_buffer_load_b64(vr, v_off[y], 0, 0);
+              ring[slot].v[4 * sub + y][0] = t[0];
+              ring[slot].v[4 * sub + y][1] = t[1];
             }
           }
         }
       };
-      auto compute = [&](int slot, int i) {
+      auto compute = [&](int slot, int step) {
         Op& x = ring[slot];
-        const int key0 = i * kStep;
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
-          if (bad[slot][sub]) {   // K and V behind a page outside the pool are zero
-#pragma unroll
-            for (int ks = 0; ks < Op::kSteps; ++ks) x.k[sub][ks] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-#pragma unroll
-              for (int z = 0; z < Op::kVWords; ++z) x.v[4 * sub + y][z] = 0u;
-          }
+        const int key0 = (i_first + step * kWaves) * kStep;
         const bool tail = key0 + kStep > all_see;
-        if (key0 + kStep > len) {
-          // slots past the entries may hold anything: 0 times a NaN of theirs would be one
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            if (key0 + 16 * (y / 4) + 4 * c + y % 4 >= len)
-#pragma unroll
-              for (int z = 0; z < Op::kVWords; ++z) x.v[y][z] = 0u;
-        }
         bf16x8 hi[kRowTiles], lo[kRowTiles];
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
@@ -286,14 +311,15 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
           }
         }
       };
-      if (i_last >= i_first) {
+      if (steps > 0) {
+        fetch_pages(0);
 #pragma unroll
-        for (int j = 0; j < kRing; ++j) issue(j, min(i_first + j * kWaves, i_last));
-        for (int i = i_first; i <= i_last; i += kRing * kWaves) {
+        for (int j = 0; j < kRing; ++j) issue(j, j);
+        for (int x = 0; x < steps; x += kRing) {
 #pragma unroll
           for (int j = 0; j < kRing; ++j) {
-            if (i + j * kWaves <= i_last) compute(j, i + j * kWaves);
-            issue(j, min(i + (j + kRing) * kWaves, i_last));
+            if (j == 0 || x + j < steps) compute(j, x + j);
+            issue(j, x + j + kRing);
           }
         }
       }
@@ -354,6 +380,10 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     }
     start += n_units;
     if (h == a.Hkv - 1) q_off += n;
+    if (start >= c1) break;   // (there are units left, so there is another segment)
+    const Segment next = segment(a, ++s);
+    len = __builtin_amdgcn_readfirstlane(next.len);
+    n = __builtin_amdgcn_readfirstlane(next.n);
   }
 }
 
@@ -369,7 +399,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   const int r = s / a.Hkv, h = s % a.Hkv, n = a.q_lens[r];
   if (mrow >= n * a.G) return;
   const int S = a.R * a.Hkv;
-  const int64_t cs = a.seg_start[s], ce = a.seg_start[s + 1], total = a.seg_start[S];
+  const int cs = a.seg_start[s], ce = a.seg_start[s + 1], total = a.seg_start[S];
   const int j = mrow / a.G, gq = mrow - j * a.G;
   const int64_t at = (int64_t)(a.q_off[r] + j) * a.Hq + h * a.G + gq;
   if (cs == ce) {
@@ -377,13 +407,14 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
     if (tid == 0 && a.lse) a.lse[at] = kNegInf;
     return;
   }
-  const int64_t wgs = total < grid ? total : grid;
-  const int first = workgroup_of(cs, total, wgs), last = workgroup_of(ce - 1, total, wgs);
+  const Shares shares(total, grid);
+  const int first = shares.holder(cs), last = shares.holder(ce - 1);
   if (first == last) return;   // written by that workgroup
   const int pieces = last - first + 1;
+  // only the first piece can be its workgroup's second
+  const int second = shares.begin(first) < cs ? 1 : 0;
   auto slot_of = [&](int p) {
-    const int wg = first + p;
-    return (2 * (int64_t)wg + (total * wg / wgs < cs ? 1 : 0)) * a.max_rows + mrow;
+    return (int64_t)(2 * (first + p) + (p == 0 ? second : 0)) * a.max_rows + mrow;
   };
   float m = kNegInf;
   for (int p = tid; p < pieces; p += kThreads) m = fmaxf(m, a.part_ml[slot_of(p)].x);
@@ -456,20 +487,25 @@ hipError_t launch_append(const AttendArgs& a, int64_t max_n, const void* k_new, 
 }
 
 hipError_t launch_attend(const AttendArgs& a, int64_t units, hipStream_t s) {
-  int64_t wgs = 2 * device_cus();
-  if (wgs > kAttendMaxWgs) wgs = kAttendMaxWgs;
-  if (wgs > units) wgs = units;
-  if (wgs < 1) wgs = 1;
-  auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(kThreads), 0, s, a);
+  int64_t wgs = 0;
+  auto run = [&](auto d, auto tiles) {
+    constexpr int D = decltype(d)::value, kTiles = decltype(tiles)::value;
+    wgs = (int64_t)Shape<D, kTiles>::kWgs * device_cus();
+    if (wgs > kAttendMaxWgs) wgs = kAttendMaxWgs;
+    if (wgs > units) wgs = units;
+    if (wgs < 1) wgs = 1;
+    hipLaunchKernelGGL((attend_kernel<D, kTiles>), dim3((unsigned)wgs), dim3(kThreads), 0, s, a);
   };
-  const int tiles = a.max_rows <= 16 ? 1 : (a.max_rows <= 32 ? 2 : 4);
-  if (a.D == 128)
-    tiles == 1 ? run(attend_kernel<128, 1>) : tiles == 2 ? run(attend_kernel<128, 2>)
-                                                         : run(attend_kernel<128, 4>);
-  else
-    tiles == 1 ? run(attend_kernel<64, 1>) : tiles == 2 ? run(attend_kernel<64, 2>)
-                                                        : run(attend_kernel<64, 4>);
+  auto run_d = [&](auto d) {
+    switch ((a.max_rows + 15) / 16) {
+      case 1: run(d, std::integral_constant<int, 1>()); break;
+      case 2: run(d, std::integral_constant<int, 2>()); break;
+      case 3: run(d, std::integral_constant<int, 3>()); break;
+      default: run(d, std::integral_constant<int, 4>()); break;
+    }
+  };
+  if (a.D == 128) run_d(std::integral_constant<int, 128>());
+  else run_d(std::integral_constant<int, 64>());
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)(a.R * a.Hkv), (unsigned)a.max_rows);
