@@ -473,8 +473,8 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
  *   causal   query j sees the entries t <= kv_lens - n_r + j (the newest tokens are the last n_r of
  *            every head); otherwise all of them.
  *   k_new, v_new  (both or neither) bf16 [sum n][Hkv][D], rows new_stride elements apart: the newest
- *            tokens' K and V, which the call first writes to the entries kv_lens - n_r + j; those
- *            below 0, and those whose page lies outside the pool, are not written.
+ *            tokens' K and V: they count as the entries kv_lens - n_r + j and are written there;
+ *            those below 0 are left out, and those whose page lies outside the pool not written.
  *   q        bf16 [sum n][Hq][D], rows q_stride elements apart (Hq * D when it stands alone; the
  *            parts of one fused projection have a larger stride).  Both strides: multiples of 8.
  *   out      bf16 [sum n][Hq][D]; lse (nullable) fp32 [sum n][Hq], natural log.

@@ -281,27 +281,33 @@ hipError_t launch_compact_inplace(const DevProblem& dp, const HostPlan& hp, void
                                   hipStream_t s);
 
 // Decode attention (actkv_attend).
-constexpr int kAttendUnit = 128;      // keys of a unit of work
-constexpr int kAttendMaxWgs = 1024;   // workgroups that share it
+constexpr int kAttendStep = 32;       // keys of a step of work
+constexpr int kAttendMaxWgs = 256;    // workgroups that share it
+constexpr int kAttendMaxWaves = 8;    // waves of a workgroup
+// KV heads that a workgroup of so many waves takes side by side
+inline int attend_head_waves(int Hkv, int waves) {
+  int w = 1;
+  while (w < waves && Hkv % (2 * w) == 0) w *= 2;
+  return w;
+}
 struct AttendArgs {
   int32_t R, Hq, Hkv, G, D, bt_stride, causal, max_rows;   // max_rows: most n * G of a request
-  int64_t num_pages, q_stride;
+  int32_t head_waves;                   // KV heads of a workgroup (chosen at launch)
+  int32_t Hkv_slots;                    // heads a partial of a workgroup holds: Hkv, with kv_lens 1
+  int64_t num_pages, q_stride, new_stride;
   float alpha;                          // sm_scale * log2(e)
   const int32_t *q_lens, *seq_lens, *kv_lens, *bt;
-  const uint16_t* q;
+  const uint16_t *q, *k_new, *v_new;
   const char* kv;
   uint16_t* out;
   float* lse;
-  int32_t* seg_start;                   // workspace [R * Hkv + 1]: units before each segment
+  int32_t* start;                       // workspace [R, with kv_lens R * Hkv, + 1]: steps before each item
   int32_t* q_off;                       // workspace [R]
-  float* part_o;                        // workspace [2 * workgroups][max_rows][D]
-  float2* part_ml;                      // workspace [2 * workgroups][max_rows]: shift and sum
+  float* part_o;                        // workspace [2 * workgroups][Hkv_slots][max_rows][D]
+  float2* part_ml;                      // workspace, the same without D: shift and sum
 };
-hipError_t launch_append(const AttendArgs& a, int64_t max_n, const void* k_new, const void* v_new,
-                         int64_t stride, hipStream_t s);
-// units: the most there can be (from the host's lengths)
-hipError_t launch_attend(const AttendArgs& a, int64_t units, hipStream_t s);
-
+// steps: the most one head can have (from the host's lengths)
+hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s);
 // Shared pages (actkv_acquire_pages and its fellows).
 constexpr int64_t kReleaseBlock = 8192;   // pages whose freed ones one workgroup lists
 inline int64_t release_blocks(int64_t num_pages) { return (num_pages + kReleaseBlock - 1) / kReleaseBlock; }

@@ -902,11 +902,11 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Decode attention: the problem's rows and units, and where its workspace lies.
+// Decode attention: the problem's rows and the steps of a head, and where its workspace lies.
 struct AttendPlan {
   HostPlan hp;
-  int64_t units = 0, max_rows = 0;
-  size_t seg_start = 0, q_off = 0, part_ml = 0, part_o = 0, total = 0;
+  int64_t steps = 0, max_rows = 0;
+  size_t start = 0, q_off = 0, part_ml = 0, part_o = 0, total = 0;
 };
 
 actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
@@ -915,14 +915,18 @@ actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   const HostPlan& hp = ap->hp;
   ap->max_rows = hp.max_n * hp.G;
   if (ap->max_rows > ACTKV_ATTEND_MAX_ROWS) return ACTKV_ERR_UNSUPPORTED;
+  // (the newest tokens may be steps of their own)
   for (int r = 0; r < hp.R; ++r)
-    ap->units += (p->seq_lens_h[r] + (int64_t)actkv::kAttendUnit - 1) / actkv::kAttendUnit * hp.Hkv;
+    ap->steps += (p->seq_lens_h[r] + (int64_t)actkv::kAttendStep - 1) / actkv::kAttendStep + 1 +
+                 p->q_lens_h[r] / actkv::kAttendStep;
   const int64_t segs = (int64_t)hp.R * hp.Hkv;
-  if (ap->units > INT32_MAX / 2 || segs > INT32_MAX / 2) return ACTKV_ERR_UNSUPPORTED;
-  const int64_t slots = 2 * (ap->units < actkv::kAttendMaxWgs ? ap->units : actkv::kAttendMaxWgs);
+  if (ap->steps * hp.Hkv > INT32_MAX / 2 || segs > INT32_MAX / 2) return ACTKV_ERR_UNSUPPORTED;
+  // two partials per workgroup and head of it
+  int64_t slots = (int64_t)actkv::kAttendMaxWgs * actkv::attend_head_waves(hp.Hkv, actkv::kAttendMaxWaves);
+  slots = 2 * (slots < ap->steps * hp.Hkv ? slots : ap->steps * hp.Hkv);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = actkv::align256(o + bytes); return at; };
-  ap->seg_start = take(sizeof(int32_t) * (size_t)(segs + 1));
+  ap->start = take(sizeof(int32_t) * (size_t)(segs + 1));
   ap->q_off = take(sizeof(int32_t) * (size_t)hp.R);
   ap->part_ml = take(2 * sizeof(float) * (size_t)(slots * ap->max_rows));
   ap->part_o = take(sizeof(float) * (size_t)(slots * ap->max_rows * hp.D));
@@ -976,21 +980,21 @@ actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_strid
   a.q_lens = p->q_lens_d;
   a.seq_lens = p->seq_lens_d;
   a.kv_lens = kv_lens;
+  a.Hkv_slots = kv_lens ? 1 : hp.Hkv;
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.new_stride = new_stride;
   a.bt = block_table;
   a.q = static_cast<const uint16_t*>(q);
   a.kv = static_cast<const char*>(kv_cache);
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
-  a.seg_start = reinterpret_cast<int32_t*>(base + ap.seg_start);
+  a.start = reinterpret_cast<int32_t*>(base + ap.start);
   a.q_off = reinterpret_cast<int32_t*>(base + ap.q_off);
   a.part_ml = reinterpret_cast<float2*>(base + ap.part_ml);
   a.part_o = reinterpret_cast<float*>(base + ap.part_o);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (k_new && hp.sum_L > 0) {
-    st = hip_status(actkv::launch_append(a, hp.max_n, k_new, v_new, new_stride, s));
-    if (st != ACTKV_OK) return st;
-  }
-  return hip_status(actkv::launch_attend(a, ap.units, s));
+  return hip_status(actkv::launch_attend(a, ap.steps, s));
 }
 
 actkv_status actkv_acquire_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
