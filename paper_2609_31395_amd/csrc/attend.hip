@@ -29,6 +29,7 @@ static_assert(kStep == 2 * kPageSize, "a step is two pages");
 // gives the same sums to rounding while nothing overflows, and a rescaling costs a pass over o.
 constexpr float kLazy = 8.0f;
 constexpr float kNegInf = -__builtin_inff();
+constexpr int kItemCost = 6;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // Waves of a workgroup (8: two on every SIMD of a CU, which a workgroup has to itself; 4 where the
@@ -60,8 +61,12 @@ __device__ __forceinline__ Item item_of(const AttendArgs& a, int x) {
   return it;
 }
 
-// Equal shares of `total` steps for at most `grid` workgroups, the first `more` of them a step larger
-// (no more workgroups than steps: each of them holds one at least).
+// What an item costs a workgroup beside its steps (its queries, page ids and the join of the waves'
+// pieces, about 4 us), in steps of a workgroup of `hw` heads side by side (0.6 us of one).
+__device__ __forceinline__ int item_cost(int hw) { return (kItemCost + hw - 1) / hw; }
+
+// Equal shares of `total` cost for at most `grid` workgroups, the first `more` of them larger by one
+// (no more workgroups than units of cost: each of them holds one at least).
 struct Shares {
   int wgs, each, more;
   __device__ __forceinline__ Shares(int total, int grid) {
@@ -70,9 +75,9 @@ struct Shares {
     more = total - wgs * each;
   }
   __device__ __forceinline__ int begin(int b) const { return b * each + min(b, more); }
-  __device__ __forceinline__ int holder(int step) const {   // the workgroup whose share it is in
+  __device__ __forceinline__ int holder(int unit) const {   // the workgroup whose share it is in
     const int large = more * (each + 1);
-    return step < large ? step / (each + 1) : more + (step - large) / each;
+    return unit < large ? unit / (each + 1) : more + (unit - large) / each;
   }
 };
 
@@ -181,13 +186,15 @@ void attend_kernel(AttendArgs a) {
   const int b = blockIdx.x / groups;
   const int h_wave = a.kv_lens ? 0 : (int)(blockIdx.x % groups) * hw + w % hw, k_wave = w / hw;
 
-  // the plan: steps and new tokens before each item (every workgroup finds its own share)
+  // the plan: cost and new tokens before each item (every workgroup finds its own share)
+  const int fixed = item_cost(hw);
+  auto cost_of = [&](const Item& i) { const int n_steps = i.steps(); return n_steps > 0 ? n_steps + fixed : 0; };
   const int per = ceil_div(items, kThreads);
   int64_t own = 0;
   Item it = {0, 0, 0};   // this thread's (last) item
   for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
     it = item_of(a, x);
-    own += ((int64_t)it.steps() << 32) + (!a.kv_lens || x % a.Hkv == 0 ? it.n : 0);
+    own += ((int64_t)cost_of(it) << 32) + (!a.kv_lens || x % a.Hkv == 0 ? it.n : 0);
   }
   int64_t all;
   const int64_t before = block_excl_scan_i64(own, scan_s, &all);
@@ -200,12 +207,12 @@ void attend_kernel(AttendArgs a) {
     int t = t_before, q = (int)before;
     for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
       if (per > 1) it = item_of(a, x);
-      const int h = a.kv_lens ? x % a.Hkv : 0, n_steps = it.steps();
+      const int h = a.kv_lens ? x % a.Hkv : 0, cost = cost_of(it);
       if (blockIdx.x == 0) {
         a.start[x] = t;
         if (h == 0) a.q_off[a.kv_lens ? x / a.Hkv : x] = q;
       }
-      if (mine && t <= c0 && c0 < t + n_steps) {
+      if (mine && t <= c0 && c0 < t + cost) {
         first_s[0] = x;
         first_s[1] = t;
         first_s[2] = h == 0 ? q : q - it.n;
@@ -213,7 +220,7 @@ void attend_kernel(AttendArgs a) {
         first_s[4] = it.cached;
         first_s[5] = it.fresh;
       }
-      t += n_steps;
+      t += cost;
       if (h == 0) q += it.n;
     }
     if (blockIdx.x == 0 && tid == 0) a.start[items] = total;
@@ -235,10 +242,12 @@ void attend_kernel(AttendArgs a) {
   for (;;) {
     const int r = a.kv_lens ? x / a.Hkv : x, h = a.kv_lens ? x % a.Hkv : h_wave;
     const int n = it.n, n_steps = it.steps(), cached_steps = it.cached_steps();
-    if (n_steps > 0) {
-      const int t0 = max(c0 - start, 0), t1 = min(c1 - start, n_steps);
+    // the workgroup's steps of the item (none where its share ends in the item's fixed cost)
+    const int t0 = max(c0 - start - fixed, 0), t1 = min(c1 - start - fixed, n_steps);
+    if (t0 < t1) {
       const bool whole = t0 == 0 && t1 == n_steps;
-      const int64_t slot = (int64_t)(2 * b + (start > c0 ? 1 : 0)) * a.Hkv_slots + (a.kv_lens ? 0 : h);
+      // a workgroup leaves at most one piece that starts its item, and one that does not
+      const int64_t slot = (int64_t)(2 * b + (t0 == 0 ? 1 : 0)) * a.Hkv_slots + (a.kv_lens ? 0 : h);
       const int rows = n * a.G, len = it.cached + it.fresh;
 
       Rows<D, kRowTiles> st;
@@ -418,6 +427,58 @@ void attend_kernel(AttendArgs a) {
           }
         }
       }
+      // the pieces of a head's key waves joined, 16 rows at a time
+      auto join_waves = [&](auto key_waves) {
+        constexpr int kW = decltype(key_waves)::value, kH = kWaves / kW > 0 ? kWaves / kW : 1;
+#pragma unroll
+        for (int rt = 0; rt < kRowTiles; ++rt) {
+          const float l = xor_sum(xor_sum(st.l[rt], 16), 32);
+          if (lane < 16) {
+            m_s[w][lane] = st.m[rt];
+            l_s[w][lane] = l;
+          }
+          __syncthreads();
+          float m = m_s[w % kH][i16];
+#pragma unroll
+          for (int k = 1; k < kW; ++k) m = fmaxf(m, m_s[w % kH + k * kH][i16]);
+          const float f = st.m[rt] == kNegInf ? 0.f : fast_exp2(st.m[rt] - m);
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int e = 0; e < kE; e += 4)
+              *reinterpret_cast<f32x4*>(&o_s[w][i16][kE * (4 * c + v) + e]) =
+                  f32x4{st.o[rt][e][v], st.o[rt][e + 1][v], st.o[rt][e + 2][v], st.o[rt][e + 3][v]} * f;
+          __syncthreads();
+          // a row's kE elements at a time, 16 threads to a row, 16 rows of each head
+          for (int y = tid; y < 256 * kH; y += kThreads) {
+            const int hh = y >> 8, row = (y >> 4) & 15, d = (y & 15) * kE, mrow = rt * 16 + row;
+            if (mrow >= rows) continue;
+            float mk[kW], mm = kNegInf, ll = 0.f, o[kE];
+#pragma unroll
+            for (int k = 0; k < kW; ++k) {
+              mk[k] = m_s[hh + k * kH][row];
+              mm = fmaxf(mm, mk[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kW; ++k)
+              ll += mk[k] == kNegInf ? 0.f : l_s[hh + k * kH][row] * fast_exp2(mk[k] - mm);
+#pragma unroll
+            for (int e = 0; e < kE; ++e) o[e] = 0.f;
+#pragma unroll 1
+            for (int k0 = 0; k0 < kW; k0 += 2)   // (two at a time: more would not fit the registers)
+#pragma unroll
+              for (int k = k0; k < k0 + 2; ++k)
+#pragma unroll
+                for (int e = 0; e < kE; e += 4) {
+                  const f32x4 v = *reinterpret_cast<const f32x4*>(&o_s[hh + k * kH][row][d + e]);
+                  o[e] += v[0]; o[e + 1] += v[1]; o[e + 2] += v[2]; o[e + 3] += v[3];
+                }
+            const int head = a.kv_lens ? h : h_wave - w % kH + hh;
+            put_row<D>(a, whole, a.kv_lens ? slot : slot - h + head, q_off, head, mrow, d, o, mm, ll);
+          }
+          __syncthreads();   // o_s and m_s are written again
+        }
+      };
       if (kw == 1) {
         // the wave's rows are the piece's: lane l holds elements 2 kE c' .. of row i
 #pragma unroll
@@ -433,49 +494,17 @@ void attend_kernel(AttendArgs a) {
             }
           }
         }
+      } else if (kw == 2) {
+        join_waves(std::integral_constant<int, 2>());
+      } else if (kw == 4) {
+        join_waves(std::integral_constant<int, 4>());
       } else {
-        // the pieces of a head's key waves joined, 16 rows at a time
-#pragma unroll
-        for (int rt = 0; rt < kRowTiles; ++rt) {
-          const float l = xor_sum(xor_sum(st.l[rt], 16), 32);
-          if (lane < 16) {
-            m_s[w][lane] = st.m[rt];
-            l_s[w][lane] = l;
-          }
-          __syncthreads();
-          float m = kNegInf;
-          for (int k = w % hw; k < kWaves; k += hw) m = fmaxf(m, m_s[k][i16]);
-          const float f = st.m[rt] == kNegInf ? 0.f : fast_exp2(st.m[rt] - m);
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-#pragma unroll
-            for (int e = 0; e < kE; e += 4)
-              *reinterpret_cast<f32x4*>(&o_s[w][i16][kE * (4 * c + v) + e]) =
-                  f32x4{st.o[rt][e][v], st.o[rt][e + 1][v], st.o[rt][e + 2][v], st.o[rt][e + 3][v]} * f;
-          __syncthreads();
-          // a row's kE elements at a time, 16 threads to a row, 16 hw rows
-          for (int y = tid; y < 256 * hw; y += kThreads) {
-            const int hh = y >> 8, row = (y >> 4) & 15, d = (y & 15) * kE, mrow = rt * 16 + row;
-            if (mrow >= rows) continue;
-            float mm = kNegInf, ll = 0.f, o[kE];
-#pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] = 0.f;
-            for (int k = hh; k < kWaves; k += hw) mm = fmaxf(mm, m_s[k][row]);
-            for (int k = hh; k < kWaves; k += hw) {
-              ll += m_s[k][row] == kNegInf ? 0.f : l_s[k][row] * fast_exp2(m_s[k][row] - mm);
-#pragma unroll
-              for (int e = 0; e < kE; ++e) o[e] += o_s[k][row][d + e];
-            }
-            const int head = a.kv_lens ? h : h_wave - w % hw + hh;
-            put_row<D>(a, whole, a.kv_lens ? slot : slot - h + head, q_off, head, mrow, d, o, mm, ll);
-          }
-          __syncthreads();   // o_s and m_s are written again
-        }
+        join_waves(std::integral_constant<int, 8>());
       }
     }
-    start += n_steps;
+    start += cost_of(it);
     if (!a.kv_lens || h == a.Hkv - 1) q_off += n;
-    if (start >= c1) break;   // (there are steps left, so there is another item)
+    if (start >= c1) break;   // (there is cost left, so there is another item)
     const Item next = item_of(a, ++x);
     it.n = __builtin_amdgcn_readfirstlane(next.n);
     it.cached = __builtin_amdgcn_readfirstlane(next.cached);
@@ -483,80 +512,107 @@ void attend_kernel(AttendArgs a) {
   }
 }
 
-// One workgroup per (request and KV head, query row): the pieces of a segment that several workgroups
-// hold, and the rows of an empty one.
+// The pieces of a segment (request and KV head) that several workgroups hold, and the rows of an empty
+// one.  kWide: a workgroup per row, for long segments in many pieces; otherwise a wave per row
+// (attend_draft, 5,120 rows of 2 or 3 pieces: ... against 15.6 us).
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 
-template <int D>
+template <int D, bool kWide>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, int grid) {
-  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes, kBatch = 8;
-  __shared__ float weight[kAttendMaxWgs];
+  constexpr int kLanes = D / 4, kBatch = 8;                      // lanes of a row of D
+  constexpr int kSpan = kWide ? kJoinThreads : 64, kGroups = kSpan / kLanes;   // threads of a row
+  __shared__ float weight[kWide ? kAttendMaxWgs : 1];
   __shared__ float red[2][kJoinWaves];
-  __shared__ __align__(16) float o_s[kGroups][D];
-  const int s = blockIdx.x, mrow = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  __shared__ __align__(16) float o_s[kWide ? kGroups : 1][D];
+  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int mrow = kWide ? (int)blockIdx.y : (int)blockIdx.y * kJoinWaves + w;
+  const int t = kWide ? tid : lane;   // within the row's threads
   const int r = s / a.Hkv, h = s % a.Hkv, n = a.q_lens[r];
-  if (mrow >= n * a.G) return;
   const int x = a.kv_lens ? s : r, groups = a.kv_lens ? 1 : a.Hkv / a.head_waves;
   const int cs = a.start[x], ce = a.start[x + 1], total = a.start[a.kv_lens ? a.R * a.Hkv : a.R];
+  const int q_off = a.q_off[r];
+  if (mrow >= n * a.G) return;
   const int j = mrow / a.G, gq = mrow - j * a.G;
-  const int64_t at = (int64_t)(a.q_off[r] + j) * a.Hq + h * a.G + gq;
+  const int64_t at = (int64_t)(q_off + j) * a.Hq + h * a.G + gq;
   if (cs == ce) {
-    if (tid < D) reinterpret_cast<uint16_t*>(a.out)[at * D + tid] = 0;
-    if (tid == 0 && a.lse) a.lse[at] = kNegInf;
+    for (int d = t; d < D; d += kSpan) reinterpret_cast<uint16_t*>(a.out)[at * D + d] = 0;
+    if (t == 0 && a.lse) a.lse[at] = kNegInf;
     return;
   }
   const Shares shares(total, grid / groups);
-  const int first = shares.holder(cs), last = shares.holder(ce - 1);
+  const int first = shares.holder(cs + item_cost(a.head_waves)), last = shares.holder(ce - 1);
   if (first == last) return;   // written by that workgroup
   const int pieces = last - first + 1;
-  // only the first piece can be its workgroup's second
-  const int second = shares.begin(first) < cs ? 1 : 0;
-  auto slot_of = [&](int p) {
-    return ((int64_t)(2 * (first + p) + (p == 0 ? second : 0)) * a.Hkv_slots + (a.kv_lens ? 0 : h)) * a.max_rows + mrow;
+  auto slot_of = [&](int p) {   // the first piece starts the item
+    return ((int64_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.Hkv_slots + (a.kv_lens ? 0 : h)) * a.max_rows + mrow;
   };
   float m = kNegInf;
-  for (int p = tid; p < pieces; p += kJoinThreads) m = fmaxf(m, a.part_ml[slot_of(p)].x);
+  for (int p = t; p < pieces; p += kSpan) m = fmaxf(m, a.part_ml[slot_of(p)].x);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = xor_max(m, d);
-  if (lane == 0) red[0][w] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  if constexpr (kWide) {
+    if (lane == 0) red[0][w] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  }
+  const int grp = t / kLanes, d4 = (t % kLanes) * 4;
   float l = 0.f;
-  for (int p = tid; p < pieces; p += kJoinThreads) {
-    const float2 ml = a.part_ml[slot_of(p)];
-    const float f = ml.x == kNegInf ? 0.f : fast_exp2(ml.x - m);
-    weight[p] = f;
-    l += ml.y * f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  // pieces p0 .. : their weights (in LDS, or one per lane), then their rows, kBatch loads in flight
+  for (int p0 = 0; p0 < pieces; p0 += kSpan) {
+    const int here = min(pieces - p0, kSpan);
+    float f = 0.f;
+    if (t < here) {
+      const float2 ml = a.part_ml[slot_of(p0 + t)];
+      f = ml.x == kNegInf ? 0.f : fast_exp2(ml.x - m);
+      l += ml.y * f;
+    }
+    if constexpr (kWide) {
+      weight[t] = f;
+      __syncthreads();
+    }
+    for (int k0 = 0; k0 < here; k0 += kGroups * kBatch) {
+      f32x4 v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        v[k] = *reinterpret_cast<const f32x4*>(
+            a.part_o + slot_of(p0 + min(k0 + k * kGroups + grp, here - 1)) * D + d4);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int p = k0 + k * kGroups + grp;
+        float g;
+        if constexpr (kWide) g = weight[min(p, kSpan - 1)];
+        else g = __shfl(f, p & 63, 64);
+        o += v[k] * (p < here ? g : 0.f);
+      }
+    }
+    if constexpr (kWide) __syncthreads();   // weight is written again
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) l = xor_sum(l, d);
-  if (lane == 0) red[1][w] = l;
-  __syncthreads();
-  l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-  const int grp = tid / kLanes, d4 = (tid % kLanes) * 4;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = grp; p0 < pieces; p0 += kGroups * kBatch) {   // kBatch loads in flight
-    f32x4 v[kBatch];
-    float f[kBatch];
+  if constexpr (kWide) {
+    if (lane == 0) red[1][w] = l;
+    *reinterpret_cast<f32x4*>(&o_s[grp][d4]) = o;
+    __syncthreads();
+    l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    if (t >= kLanes) return;
+    o = *reinterpret_cast<const f32x4*>(&o_s[0][d4]);
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int p = p0 + k * kGroups;
-      f[k] = p < pieces ? weight[p] : 0.f;
-      v[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot_of(min(p, pieces - 1)) * D + d4);
-    }
+    for (int k = 1; k < kGroups; ++k) o += *reinterpret_cast<const f32x4*>(&o_s[k][d4]);
+  } else {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) o += v[k] * f[k];
+    for (int d = 32; d >= kLanes; d >>= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = xor_sum(o[e], d);
+    if (t >= kLanes) return;
   }
-  *reinterpret_cast<f32x4*>(&o_s[grp][d4]) = o;
-  __syncthreads();
-  if (tid < D) {
-    float v = 0.f;
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
-    for (int k = 0; k < kGroups; ++k) v += o_s[k][tid];
-    reinterpret_cast<__bf16*>(a.out)[at * D + tid] = (__bf16)(l > 0.f ? v / l : 0.f);
-    if (tid == 0 && a.lse) a.lse[at] = m == kNegInf ? kNegInf : (m + __log2f(l)) * kLn2;
-  }
+  for (int e = 0; e < 4; ++e) reinterpret_cast<__bf16*>(a.out)[at * D + d4 + e] = (__bf16)(o[e] * inv);
+  if (t == 0 && a.lse) a.lse[at] = m == kNegInf ? kNegInf : (m + __log2f(l)) * kLn2;
 }
+
+static_assert(kAttendMaxWgs <= kJoinThreads, "a weight per thread");
 
 hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s) {
   int64_t wgs = 0;
@@ -586,11 +642,15 @@ hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s) {
   else run_d(std::integral_constant<int, 64>());
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)(a.R * a.Hkv), (unsigned)a.max_rows);
-  if (a.D == 128)
-    hipLaunchKernelGGL(attend_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, a, (int)wgs);
-  else
-    hipLaunchKernelGGL(attend_join_kernel<64>, grid, dim3(kJoinThreads), 0, s, a, (int)wgs);
+  // more than 16 pieces to a segment in the mean: a workgroup per row
+  const int64_t gangs = a.kv_lens ? wgs : wgs / (a.Hkv / a.head_waves);
+  const bool wide = gangs > 16 * (int64_t)(a.kv_lens ? a.R * a.Hkv : a.R);
+  const dim3 grid((unsigned)(a.R * a.Hkv), (unsigned)(wide ? a.max_rows : (a.max_rows + kJoinWaves - 1) / kJoinWaves));
+  auto join = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kJoinThreads), 0, s, a, (int)wgs);
+  };
+  if (a.D == 128) wide ? join(attend_join_kernel<128, true>) : join(attend_join_kernel<128, false>);
+  else wide ? join(attend_join_kernel<64, true>) : join(attend_join_kernel<64, false>);
   return hipGetLastError();
 }
 
