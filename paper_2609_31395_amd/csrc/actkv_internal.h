@@ -283,12 +283,25 @@ hipError_t launch_compact_inplace(const DevProblem& dp, const HostPlan& hp, void
 // Decode attention (actkv_attend).
 constexpr int kAttendStep = 32;       // keys of a step of work
 constexpr int kAttendMaxWgs = 256;    // workgroups that share it
-constexpr int kAttendMaxWaves = 8;    // waves of a workgroup
-// KV heads that a workgroup of so many waves takes side by side
-inline int attend_head_waves(int Hkv, int waves) {
-  int w = 1;
-  while (w < waves && Hkv % (2 * w) == 0) w *= 2;
-  return w;
+// Waves of a workgroup, by head size and the most query rows of a KV head.
+__host__ __device__ constexpr int attend_waves(int D, int64_t rows) { return D == 128 && rows > 32 ? 4 : 8; }
+// KV heads that a workgroup takes side by side where all heads of a request have the same entries:
+// the power of two with the least traffic.  Each head of a workgroup leaves a partial, written and read
+// again; and the fewer heads of a page's slots are read together, the less the memory gives: of its
+// best rate 15% less for 128 bytes of a slot, 6% for 256, 2% for 512 (measured: 16 x 11,500 entries of 8
+// heads of 64, one token, 84.7, 74.7, 73.9 and 74.1 us with 1, 2, 4 and 8 heads, five tokens 96.3, 86.5,
+// 87.8 and 90.2; 4 heads of 128, 32 x 35,000 entries 410, 393 and 386, 1 x 35,000 21.5, 21.9 and 23.8).
+inline int attend_head_waves(int Hkv, int D, int64_t rows, int64_t entries) {
+  const double bytes = 4.0 * D * Hkv * (double)entries;
+  int best = 1;
+  double least = 0;
+  for (int w = 1; w <= attend_waves(D, rows) && Hkv % w == 0; w *= 2) {
+    const int span = 2 * D * w;
+    const double loss = span < 256 ? 0.15 : span < 512 ? 0.06 : span < 1024 ? 0.02 : 0.0;
+    const double cost = bytes * loss + 2.0 * kAttendMaxWgs * w * rows * (4 * D + 8);
+    if (w == 1 || cost < least) { best = w; least = cost; }
+  }
+  return best;
 }
 struct AttendArgs {
   int32_t R, Hq, Hkv, G, D, bt_stride, causal, max_rows;   // max_rows: most n * G of a request

@@ -906,6 +906,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 struct AttendPlan {
   HostPlan hp;
   int64_t steps = 0, max_rows = 0;
+  int head_waves = 1;
   size_t start = 0, q_off = 0, part_ml = 0, part_o = 0, total = 0;
 };
 
@@ -915,14 +916,13 @@ actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   const HostPlan& hp = ap->hp;
   ap->max_rows = hp.max_n * hp.G;
   if (ap->max_rows > ACTKV_ATTEND_MAX_ROWS) return ACTKV_ERR_UNSUPPORTED;
-  // (the newest tokens may be steps of their own)
   for (int r = 0; r < hp.R; ++r)
-    ap->steps += (p->seq_lens_h[r] + (int64_t)actkv::kAttendStep - 1) / actkv::kAttendStep + 1 +
-                 p->q_lens_h[r] / actkv::kAttendStep;
+    ap->steps += (p->seq_lens_h[r] + (int64_t)actkv::kAttendStep - 1) / actkv::kAttendStep;
   const int64_t segs = (int64_t)hp.R * hp.Hkv;
   if (ap->steps * hp.Hkv > INT32_MAX / 2 || segs > INT32_MAX / 2) return ACTKV_ERR_UNSUPPORTED;
   // two partials per workgroup and head of it
-  int64_t slots = (int64_t)actkv::kAttendMaxWgs * actkv::attend_head_waves(hp.Hkv, actkv::kAttendMaxWaves);
+  ap->head_waves = actkv::attend_head_waves(hp.Hkv, hp.D, ap->max_rows, hp.sum_L);
+  int64_t slots = (int64_t)actkv::kAttendMaxWgs * ap->head_waves;
   slots = 2 * (slots < ap->steps * hp.Hkv ? slots : ap->steps * hp.Hkv);
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = actkv::align256(o + bytes); return at; };
@@ -981,6 +981,7 @@ actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_strid
   a.seq_lens = p->seq_lens_d;
   a.kv_lens = kv_lens;
   a.Hkv_slots = kv_lens ? 1 : hp.Hkv;
+  a.head_waves = kv_lens ? 1 : ap.head_waves;
   a.k_new = static_cast<const uint16_t*>(k_new);
   a.v_new = static_cast<const uint16_t*>(v_new);
   a.new_stride = new_stride;

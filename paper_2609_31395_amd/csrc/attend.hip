@@ -11,9 +11,8 @@
 // over its entries, x_t = sm_scale log2(e) q.k_t.  Two pieces join as m = max(m1, m2),
 // l = l1 2^(m1 - m) + l2 2^(m2 - m) and the same for o; out = o / l, LSE = (m + log2 l) ln 2.
 //
-// The newest tokens' own K and V, where the call brings them, are steps of their own behind the
-// cached ones, read from where the call has them; the wave that takes such a step also writes it to
-// the cache, which nobody reads there in this call.
+// The newest tokens' own K and V, where the call brings them, are read from where the call has them,
+// by the wave that also writes them to the cache, where nobody reads them in this call.
 #include <type_traits>
 
 #include "device_common.hpp"
@@ -32,23 +31,22 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr int kItemCost = 6;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Waves of a workgroup (8: two on every SIMD of a CU, which a workgroup has to itself; 4 where the
-// rows' registers leave room for one), and the steps of K and V that a wave has in flight.
+// Waves of a workgroup, which has a CU to itself: two on every SIMD, or one where the rows' registers
+// leave no room for two.  A wave has one step in flight; two or four of them, or two workgroups to a
+// CU, were no faster at any size (attend_batch the same; 64-element heads 78 against 73.5 us).
 template <int D, int kRowTiles>
 struct Shape {
-  static constexpr int kWaves = kRowTiles > (D == 128 ? 2 : 3) ? 4 : 8;
+  static constexpr int kWaves = attend_waves(D, 16 * kRowTiles);
   static constexpr int kThreads = kWaves * 64;
-  static_assert(kWaves <= kAttendMaxWaves, "the workspace holds their partials");
-  static constexpr int kRing = D == 128 ? (kRowTiles == 1 ? 2 : 1) : (kRowTiles == 1 ? 4 : kRowTiles == 2 ? 2 : 1);
 };
 
 // A work item: a request, or, with kv_lens, a (request, KV head) pair.  Its new tokens, its entries
-// that lie in the cache already and those that the call brings, and its steps (none without a new
-// token).
+// that lie in the cache already and those that the call brings, and its steps: those of the cached
+// entries, of which the last takes the others as well (none without a new token).
 struct Item {
   int n, cached, fresh;
   __device__ __forceinline__ int cached_steps() const { return n > 0 ? ceil_div(cached, kStep) : 0; }
-  __device__ __forceinline__ int steps() const { return n > 0 ? cached_steps() + ceil_div(fresh, kStep) : 0; }
+  __device__ __forceinline__ int steps() const { return max(cached_steps(), n > 0 && fresh > 0 ? 1 : 0); }
 };
 __device__ __forceinline__ Item item_of(const AttendArgs& a, int x) {
   const int r = a.kv_lens ? x / a.Hkv : x;
@@ -63,7 +61,7 @@ __device__ __forceinline__ Item item_of(const AttendArgs& a, int x) {
 
 // What an item costs a workgroup beside its steps (its queries, page ids and the join of the waves'
 // pieces, about 4 us), in steps of a workgroup of `hw` heads side by side (0.6 us of one).
-__device__ __forceinline__ int item_cost(int hw) { return (kItemCost + hw - 1) / hw; }
+__device__ __forceinline__ int item_cost(int hw) { return kItemCost / hw; }
 
 // Equal shares of `total` cost for at most `grid` workgroups, the first `more` of them larger by one
 // (no more workgroups than units of cost: each of them holds one at least).
@@ -80,6 +78,13 @@ struct Shares {
     return unit < large ? unit / (each + 1) : more + (unit - large) / each;
   }
 };
+
+// v, from where the compiler cannot trace it back: what is computed from it is computed there, and not
+// held in registers across a loop before it.
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
 __device__ __forceinline__ float xor_max(float v, int d) { return fmaxf(v, __shfl_xor(v, d, 64)); }
 __device__ __forceinline__ float xor_sum(float v, int d) { return v + __shfl_xor(v, d, 64); }
@@ -99,22 +104,26 @@ struct Operands {
   uint32_t v[8][kVWords];
 };
 
-// A page's operands: K and V rows from kp and vp on, `bytes` of each; the lane's places in k_off, v_off.
+// A page's operands: `bytes` of K or V rows from p on; the lane's places in them.
 template <int D>
-__device__ __forceinline__ void load_page(Operands<D>& op, int sub, const char* kp, const char* vp, int bytes,
-                                          uint32_t k_off, const uint32_t (&v_off)[4]) {
-  const __amdgpu_buffer_rsrc_t kr = buffer_over(kp, bytes), vr = buffer_over(vp, bytes);
+__device__ __forceinline__ void load_k(Operands<D>& op, int sub, const char* p, int bytes, uint32_t off) {
+  const __amdgpu_buffer_rsrc_t rs = buffer_over(p, bytes);
 #pragma unroll
   for (int ks = 0; ks < Operands<D>::kSteps; ++ks)
-    op.k[sub][ks] = __builtin_amdgcn_raw_buffer_load_b128(kr, k_off + 64 * ks, 0, 0);
+    op.k[sub][ks] = __builtin_amdgcn_raw_buffer_load_b128(rs, off + 64 * ks, 0, 0);
+}
+template <int D>
+__device__ __forceinline__ void load_v(Operands<D>& op, int sub, const char* p, int bytes,
+                                       const uint32_t (&off)[4]) {
+  const __amdgpu_buffer_rsrc_t rs = buffer_over(p, bytes);
 #pragma unroll
   for (int y = 0; y < 4; ++y) {
     if constexpr (D == 128) {
-      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(vr, v_off[y], 0, 0);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(rs, off[y], 0, 0);
 #pragma unroll
       for (int z = 0; z < 4; ++z) op.v[4 * sub + y][z] = v[z];
     } else {
-      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(vr, v_off[y], 0, 0);
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, off[y], 0, 0);
       op.v[4 * sub + y][0] = v[0];
       op.v[4 * sub + y][1] = v[1];
     }
@@ -172,7 +181,7 @@ __global__ __launch_bounds__((Shape<D, kRowTiles>::kThreads), (Shape<D, kRowTile
 void attend_kernel(AttendArgs a) {
   using Op = Operands<D>;
   using Sh = Shape<D, kRowTiles>;
-  constexpr int kE = D / 16, kRing = Sh::kRing, kWaves = Sh::kWaves, kThreads = Sh::kThreads;
+  constexpr int kE = D / 16, kWaves = Sh::kWaves, kThreads = Sh::kThreads;
   constexpr int kOStride = D + 4;
   __shared__ __align__(16) float o_s[kWaves][16][kOStride];
   __shared__ float m_s[kWaves][16], l_s[kWaves][16];
@@ -275,15 +284,14 @@ void attend_kernel(AttendArgs a) {
       uint32_t v_off[4];   // (in the lane's offset: the bounds check takes a scalar one off the size)
 #pragma unroll
       for (int y = 0; y < 4; ++y) v_off[y] = (uint32_t)((4 * c + y) * row_bytes + 2 * kE * i16);
-      Op ring[kRing];
+      Op op;
       // this wave's steps: t_first and every kw-th from there, `steps` of them in the cache
       const int t_first = t0 + k_wave;
       const int steps = max(ceil_div(min(t1, cached_steps) - t_first, kw), 0);
       // Their pages, 32 steps at a time: lane l holds the id of page l % 2 of step l / 2 and how many
       // bytes of it, from this head's first row on, hold entries.  Loads past those bytes read as
       // zero and move nothing: the slots behind the entries (which may hold anything, and 0 times a
-      // NaN of theirs would be one), pages outside the pool, and steps past the wave's last, which
-      // are issued like the others so that every wait counts the same loads.
+      // NaN of theirs would be one), and pages outside the pool.
       int32_t page_next = 0, page_now = 0, bytes_now = 0;
       auto fetch_pages = [&](int y) {
         page_next = bt_row[max(min(2 * (t_first + (y + (lane >> 1)) * kw) + (lane & 1), pages - 1), 0)];
@@ -295,21 +303,25 @@ void attend_kernel(AttendArgs a) {
         page_now = ok ? page_next : 0;
         bytes_now = ok ? (held - 1) * row_bytes + 2 * D : 0;
       };
-      auto issue = [&](int at, int step) {
+      auto issue = [&](int step) {
         if ((step & 31) == 0) {
           take_pages(step);
           fetch_pages(step + 32);
         }
+        const char* at[2];
+        int bytes[2];
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
-          const int64_t page = __builtin_amdgcn_readlane(page_now, 2 * (step & 31) + sub);
-          const int bytes = __builtin_amdgcn_readlane(bytes_now, 2 * (step & 31) + sub);
-          const char* kp = k_head + page * page_bytes;
-          load_page<D>(ring[at], sub, kp, kp + v_plane, bytes, k_off, v_off);
+          at[sub] = k_head + __builtin_amdgcn_readlane(page_now, 2 * (step & 31) + sub) * page_bytes;
+          bytes[sub] = __builtin_amdgcn_readlane(bytes_now, 2 * (step & 31) + sub);
         }
+        load_k<D>(op, 0, at[0], bytes[0], k_off);
+        load_k<D>(op, 1, at[1], bytes[1], k_off);
+        load_v<D>(op, 0, at[0] + v_plane, bytes[0], v_off);
+        load_v<D>(op, 1, at[1] + v_plane, bytes[1], v_off);
       };
       // the new tokens of a step, as loaded, to their places in the cache
-      auto write_new = [&](const Op& op, int j0) {
+      auto write_new = [&](int j0, int c, int i16) {
         char* kv = const_cast<char*>(k_head);
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
@@ -339,23 +351,27 @@ void attend_kernel(AttendArgs a) {
           }
         }
       };
+      f32x4 acc[kRowTiles][2];
+      auto scores = [&]() {
+#pragma unroll
+        for (int rt = 0; rt < kRowTiles; ++rt)
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            acc[rt][sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < Op::kSteps; ++ks)
+              acc[rt][sub] = mfma16(as_bf16x8(op.k[sub][ks]), st.q[rt][ks], acc[rt][sub]);
+          }
+      };
       // 32 entries from key0 on, of which those below `end` count
-      auto compute = [&](const Op& op, int key0, int end) {
+      auto add = [&](int key0, int end) {
         const bool tail = key0 + kStep > min(all_see, end);
         bf16x8 hi[kRowTiles], lo[kRowTiles];
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
-          f32x4 acc[2];
-#pragma unroll
-          for (int sub = 0; sub < 2; ++sub) {
-            acc[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < Op::kSteps; ++ks)
-              acc[sub] = mfma16(as_bf16x8(op.k[sub][ks]), st.q[rt][ks], acc[sub]);
-          }
           float y[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = acc[k / 4][k % 4];
+          for (int k = 0; k < 8; ++k) y[k] = acc[rt][k / 4][k % 4];
           if (tail) {
             const int last = min(st.last[rt], end);
 #pragma unroll
@@ -399,58 +415,57 @@ void attend_kernel(AttendArgs a) {
         }
       };
       if (steps > 0) fetch_pages(0);
-      // the wave's steps of new tokens
-      for (int t = t_first + steps * kw; t < t1; t += kw) {
-        const int j0 = (t - cached_steps) * kStep, new_bytes = (int)(a.new_stride * 2);
-        uint32_t vo[4];
+      // the newest tokens' own rows, by the wave that has (or would have) the last cached step
+      if (it.fresh > 0 && t1 == n_steps && t0 < t1 && (t1 - 1 - t0) % kw == k_wave)
+        for (int j0 = 0; j0 < it.fresh; j0 += kStep) {
+          const int new_bytes = (int)(a.new_stride * 2);
+          const int l2 = opaque(lane), c = l2 >> 4, i16 = l2 & 15;
+          uint32_t off[4];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) vo[y] = (uint32_t)((4 * c + y) * new_bytes + 2 * kE * i16);
+          for (int y = 0; y < 4; ++y) off[y] = (uint32_t)((4 * c + y) * new_bytes + 2 * kE * i16);
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          const int j = j0 + sub * kPageSize, held = min(it.fresh - j, kPageSize);
-          const int64_t at = ((int64_t)q_off + n - it.fresh + j) * a.new_stride + h * D;
-          load_page<D>(ring[0], sub, reinterpret_cast<const char*>(a.k_new + at),
-                       reinterpret_cast<const char*>(a.v_new + at),
-                       held > 0 ? (held - 1) * new_bytes + 2 * D : 0, (uint32_t)(i16 * new_bytes + 16 * c), vo);
-        }
-        write_new(ring[0], j0);
-        compute(ring[0], it.cached + j0, len);
-      }
-      if (steps > 0) {
-#pragma unroll
-        for (int j = 0; j < kRing; ++j) issue(j, j);
-        for (int y = 0; y < steps; y += kRing) {
-#pragma unroll
-          for (int j = 0; j < kRing; ++j) {
-            if (j == 0 || y + j < steps) compute(ring[j], (t_first + (y + j) * kw) * kStep, it.cached);
-            issue(j, y + j + kRing);
+          for (int sub = 0; sub < 2; ++sub) {
+            const int j = j0 + sub * kPageSize, held = min(it.fresh - j, kPageSize);
+            const int64_t at = ((int64_t)q_off + n - it.fresh + j) * a.new_stride + h * D;
+            const int bytes = held > 0 ? (held - 1) * new_bytes + 2 * D : 0;
+            load_k<D>(op, sub, reinterpret_cast<const char*>(a.k_new + at), bytes,
+                      (uint32_t)(i16 * new_bytes + 16 * c));
+            load_v<D>(op, sub, reinterpret_cast<const char*>(a.v_new + at), bytes, off);
           }
+          write_new(j0, c, i16);
+          scores();
+          add(it.cached + j0, len);
         }
+      for (int step = 0; step < steps; ++step) {
+        issue(step);
+        scores();
+        add((t_first + step * kw) * kStep, it.cached);
       }
+      const int tid2 = opaque(tid), lane2 = tid2 & 63, c2 = lane2 >> 4, i2 = lane2 & 15;
       // the pieces of a head's key waves joined, 16 rows at a time
       auto join_waves = [&](auto key_waves) {
         constexpr int kW = decltype(key_waves)::value, kH = kWaves / kW > 0 ? kWaves / kW : 1;
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
           const float l = xor_sum(xor_sum(st.l[rt], 16), 32);
-          if (lane < 16) {
-            m_s[w][lane] = st.m[rt];
-            l_s[w][lane] = l;
+          if (lane2 < 16) {
+            m_s[w][lane2] = st.m[rt];
+            l_s[w][lane2] = l;
           }
           __syncthreads();
-          float m = m_s[w % kH][i16];
+          float m = m_s[w % kH][i2];
 #pragma unroll
-          for (int k = 1; k < kW; ++k) m = fmaxf(m, m_s[w % kH + k * kH][i16]);
+          for (int k = 1; k < kW; ++k) m = fmaxf(m, m_s[w % kH + k * kH][i2]);
           const float f = st.m[rt] == kNegInf ? 0.f : fast_exp2(st.m[rt] - m);
 #pragma unroll
           for (int v = 0; v < 4; ++v)
 #pragma unroll
             for (int e = 0; e < kE; e += 4)
-              *reinterpret_cast<f32x4*>(&o_s[w][i16][kE * (4 * c + v) + e]) =
+              *reinterpret_cast<f32x4*>(&o_s[w][i2][kE * (4 * c2 + v) + e]) =
                   f32x4{st.o[rt][e][v], st.o[rt][e + 1][v], st.o[rt][e + 2][v], st.o[rt][e + 3][v]} * f;
           __syncthreads();
           // a row's kE elements at a time, 16 threads to a row, 16 rows of each head
-          for (int y = tid; y < 256 * kH; y += kThreads) {
+          for (int y = tid2; y < 256 * kH; y += kThreads) {
             const int hh = y >> 8, row = (y >> 4) & 15, d = (y & 15) * kE, mrow = rt * 16 + row;
             if (mrow >= rows) continue;
             float mk[kW], mm = kNegInf, ll = 0.f, o[kE];
@@ -480,17 +495,17 @@ void attend_kernel(AttendArgs a) {
         }
       };
       if (kw == 1) {
-        // the wave's rows are the piece's: lane l holds elements 2 kE c' .. of row i
+        // the wave's rows are the piece's: lane2 l holds elements 2 kE c' .. of row i
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
           const float l = xor_sum(xor_sum(st.l[rt], 16), 32);
-          if (rt * 16 + i16 < rows) {
+          if (rt * 16 + i2 < rows) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               float o[kE];
 #pragma unroll
               for (int e = 0; e < kE; ++e) o[e] = st.o[rt][e][v];
-              put_row<D>(a, whole, slot, q_off, h, rt * 16 + i16, kE * (4 * c + v), o, st.m[rt], l);
+              put_row<D>(a, whole, slot, q_off, h, rt * 16 + i2, kE * (4 * c2 + v), o, st.m[rt], l);
             }
           }
         }
@@ -521,7 +536,7 @@ template <int D, bool kWide>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a, int grid) {
   constexpr int kLanes = D / 4, kBatch = 8;                      // lanes of a row of D
   constexpr int kSpan = kWide ? kJoinThreads : 64, kGroups = kSpan / kLanes;   // threads of a row
-  __shared__ float weight[kWide ? kAttendMaxWgs : 1];
+  __shared__ float weight[kWide ? kJoinThreads : 1];
   __shared__ float red[2][kJoinWaves];
   __shared__ __align__(16) float o_s[kWide ? kGroups : 1][D];
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -547,36 +562,41 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
     return ((int64_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * a.Hkv_slots + (a.kv_lens ? 0 : h)) * a.max_rows + mrow;
   };
   float m = kNegInf;
-  for (int p = t; p < pieces; p += kSpan) m = fmaxf(m, a.part_ml[slot_of(p)].x);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) m = xor_max(m, d);
-  if constexpr (kWide) {
-    if (lane == 0) red[0][w] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  }
   const int grp = t / kLanes, d4 = (t % kLanes) * 4;
   float l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  // pieces p0 .. : their weights (in LDS, or one per lane), then their rows, kBatch loads in flight
+  // kSpan pieces at a time: the first kBatch rows of a group's set out before the pieces' weights (in
+  // LDS, or one per lane) are known
   for (int p0 = 0; p0 < pieces; p0 += kSpan) {
     const int here = min(pieces - p0, kSpan);
-    float f = 0.f;
-    if (t < here) {
-      const float2 ml = a.part_ml[slot_of(p0 + t)];
-      f = ml.x == kNegInf ? 0.f : fast_exp2(ml.x - m);
-      l += ml.y * f;
+    f32x4 v[kBatch];
+    auto load_rows = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        v[k] = *reinterpret_cast<const f32x4*>(
+            a.part_o + slot_of(p0 + min(k0 + k * kGroups + grp, here - 1)) * D + d4);
+    };
+    const float2 ml = t < here ? a.part_ml[slot_of(p0 + t)] : make_float2(kNegInf, 0.f);
+    load_rows(0);
+    if (p0 == 0) {   // the row's shift; past kSpan pieces, from all of them
+      m = ml.x;
+      for (int p = t + kSpan; p < pieces; p += kSpan) m = fmaxf(m, a.part_ml[slot_of(p)].x);
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) m = xor_max(m, d);
+      if constexpr (kWide) {
+        if (lane == 0) red[0][w] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+      }
     }
+    const float f = ml.x == kNegInf ? 0.f : fast_exp2(ml.x - m);
+    l += ml.y * f;
     if constexpr (kWide) {
       weight[t] = f;
       __syncthreads();
     }
     for (int k0 = 0; k0 < here; k0 += kGroups * kBatch) {
-      f32x4 v[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k)
-        v[k] = *reinterpret_cast<const f32x4*>(
-            a.part_o + slot_of(p0 + min(k0 + k * kGroups + grp, here - 1)) * D + d4);
+      if (k0 > 0) load_rows(k0);
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const int p = k0 + k * kGroups + grp;
@@ -612,15 +632,12 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a,
   if (t == 0 && a.lse) a.lse[at] = m == kNegInf ? kNegInf : (m + __log2f(l)) * kLn2;
 }
 
-static_assert(kAttendMaxWgs <= kJoinThreads, "a weight per thread");
-
 hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s) {
   int64_t wgs = 0;
   auto run = [&](auto d, auto tiles) {
     constexpr int D = decltype(d)::value, kTiles = decltype(tiles)::value;
     using Sh = Shape<D, kTiles>;
-    a.head_waves = a.kv_lens ? 1 : attend_head_waves(a.Hkv, Sh::kWaves);
-    // a workgroup per CU (8 waves; 4 that take a SIMD each), at most one per step of a head
+    // a workgroup per CU, at most one per step
     const int groups = a.kv_lens ? 1 : a.Hkv / a.head_waves;
     wgs = device_cus();
     if (wgs > kAttendMaxWgs) wgs = kAttendMaxWgs;
