@@ -503,16 +503,18 @@ actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_strid
  * actkv_acquire_pages: refs[page] += 1 for each of the n entries of pages.
  * actkv_release_pages: refs[page] -= 1 for each of the n entries, never below 0; freed, int32 [n],
  * receives the pages whose count came to 0, ascending, then -1; num_freed (device int32) their
- * number.  A page that had no holder before is not listed.  workspace: at least the bytes that
- * actkv_release_workspace reports (host only).
+ * number.  A page that had no holder before is not listed.  row_len: the list is rows of so many
+ * entries (0: one row), which matters to speed alone: rows that name the same page in the same place
+ * one after another, as those of a request's branches do, count it off together.  workspace: at
+ * least the bytes that actkv_release_workspace reports (host only).
  * Entries outside [0, num_pages) (the -1 of a block-table row's end) are passed over; a page may be
  * listed several times.  pages and freed must not overlap.
  */
 actkv_status actkv_acquire_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
                                  void* stream);
 actkv_status actkv_release_workspace(int64_t n, int64_t num_pages, size_t* workspace_bytes);
-actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
-                                 int32_t* freed, int32_t* num_freed, void* workspace,
+actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t row_len, int64_t num_pages,
+                                 int32_t* refs, int32_t* freed, int32_t* num_freed, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
 /*

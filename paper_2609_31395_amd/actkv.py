@@ -104,7 +104,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.actkv_attend.argtypes = [P, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
     lib.actkv_acquire_pages.argtypes = [vp, i64, i64, vp, vp]
     lib.actkv_release_workspace.argtypes = [i64, i64, psz]
-    lib.actkv_release_pages.argtypes = [vp, i64, i64, vp, vp, vp, vp, sz, vp]
+    lib.actkv_release_pages.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.actkv_fork_pages.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, i64, vp, vp, vp, i64, vp,
                                      vp]
     lib.actkv_token_logprobs_workspace.argtypes = [i64, i64, i32, psz]
@@ -1042,8 +1042,9 @@ def release_workspace(num_pages: int, n: int, device="cuda") -> torch.Tensor:
 def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch.Tensor] = None,
                   num_freed: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                   stream=None):
-    """refs[page] -= 1 for every entry of pages; returns (freed, num_freed): the pages whose count
-    came to 0, ascending, then -1 (as many values as pages), and their number (int32 [1])."""
+    """refs[page] -= 1 for every entry of pages (a list, or rows of a block table); returns (freed,
+    num_freed): the pages whose count came to 0, ascending, then -1 (as many values as pages), and
+    their number (int32 [1])."""
     lib = load_library()
     seen: list = []
     if pages is None:
@@ -1066,8 +1067,8 @@ def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch
             num_freed = on.result((1,), torch.int32)
         ws = on.scratch(need) if ws is None else ws
         _check("actkv_release_pages", lib.actkv_release_pages(
-            _ptr(pages), n, refs.numel(), _ptr(refs), _ptr(freed), _ptr(num_freed), _ptr(ws),
-            _ws_bytes(ws), on.handle))
+            _ptr(pages), n, int(pages.shape[-1]) if pages.dim() > 1 else 0, refs.numel(), _ptr(refs),
+            _ptr(freed), _ptr(num_freed), _ptr(ws), _ws_bytes(ws), on.handle))
     return freed, num_freed
 
 

@@ -323,18 +323,21 @@ struct AttendArgs {
 hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s);
 // Shared pages (actkv_acquire_pages and its fellows).
 constexpr int64_t kReleaseBlock = 8192;   // pages whose freed ones one workgroup lists
+constexpr int kReleaseRows = 8;           // rows of a list whose entries of a column one thread takes
+constexpr int kReleaseSmall = 1024;       // entries that one workgroup releases by itself
 inline int64_t release_blocks(int64_t num_pages) { return (num_pages + kReleaseBlock - 1) / kReleaseBlock; }
 hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t max_copied, int32_t bt_stride,
                        int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
                        const int32_t* free_pages, int32_t* refs, hipStream_t s);
 hipError_t launch_acquire(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
                           hipStream_t s);
-// words: of the bitmap and the blocks' counts behind it, cleared first
-hipError_t launch_release(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
-                          int32_t* freed, int32_t* num_freed, uint32_t* bits, uint32_t* counts,
-                          int64_t words, hipStream_t s);
-// Token log probabilities: chunks of kConfChunkLogits logits, conf_splits(vocab) to a row; stats holds
-// 3 floats and top k keys per chunk.
+hipError_t launch_release(const int32_t* pages, int64_t n, int64_t row_len, int64_t num_pages,
+                          int32_t* refs, int32_t* freed, int32_t* num_freed, uint32_t* bits,
+                          uint32_t* counts, hipStream_t s);
+// Token log probabilities: logprobs_splits chunks to a row (at most 64); stats holds 3 floats and top
+// k keys per chunk.
+constexpr int kLogprobsChunk = 16384, kLogprobsSmallChunk = 4096;
+int logprobs_splits(int64_t rows, int64_t vocab, int k);
 hipError_t launch_token_logprobs(const void* logits, int type, int64_t rows, int64_t vocab,
                                  int64_t row_stride, const int64_t* tokens, int k, float* logprobs,
                                  float* entropy, int64_t* top_tokens, float* top_logprobs,

@@ -1009,7 +1009,8 @@ actkv_status actkv_acquire_pages(const int32_t* pages, int64_t n, int64_t num_pa
 namespace {
 actkv_status check_release(int64_t n, int64_t num_pages) {
   if (n < 0 || num_pages <= 0) return ACTKV_ERR_INVALID_ARGUMENT;
-  if (num_pages > INT32_MAX) return ACTKV_ERR_UNSUPPORTED;   // page ids are int32
+  // page ids and the number of freed pages are int32
+  if (num_pages > INT32_MAX || n > (INT64_C(1) << 36)) return ACTKV_ERR_UNSUPPORTED;
   return ACTKV_OK;
 }
 int64_t release_words(int64_t num_pages) {
@@ -1024,19 +1025,22 @@ actkv_status actkv_release_workspace(int64_t n, int64_t num_pages, size_t* works
   return ACTKV_OK;
 }
 
-actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
-                                 int32_t* freed, int32_t* num_freed, void* workspace,
+actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t row_len, int64_t num_pages,
+                                 int32_t* refs, int32_t* freed, int32_t* num_freed, void* workspace,
                                  size_t workspace_bytes, void* stream) {
   const actkv_status st = check_release(n, num_pages);
   if (st != ACTKV_OK) return st;
+  if (row_len < 0) return ACTKV_ERR_INVALID_ARGUMENT;
+  // (shorter rows leave most of a workgroup idle)
+  if (row_len < 64 || row_len > n) row_len = n;
   if (!num_freed || (n > 0 && (!pages || !refs || !freed)) || (pages && pages == freed))
     return ACTKV_ERR_INVALID_ARGUMENT;
   const int64_t words = release_words(num_pages);
   if (workspace_bytes < sizeof(uint32_t) * (size_t)words) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3)) return ACTKV_ERR_INVALID_ARGUMENT;
   uint32_t* bits = static_cast<uint32_t*>(workspace);
-  return hip_status(actkv::launch_release(pages, n, num_pages, refs, freed, num_freed, bits,
-                                          bits + (num_pages + 31) / 32, words,
+  return hip_status(actkv::launch_release(pages, n, row_len, num_pages, refs, freed, num_freed, bits,
+                                          bits + (num_pages + 31) / 32,
                                           static_cast<hipStream_t>(stream)));
 }
 
@@ -1088,18 +1092,15 @@ actkv_status check_logprobs(int64_t rows, int64_t vocab, int32_t top_k) {
   if (rows > INT32_MAX / actkv::kConfMaxSplits) return ACTKV_ERR_UNSUPPORTED;
   return ACTKV_OK;
 }
-size_t logprobs_stats(int64_t rows, int64_t vocab) {
-  return actkv::align256(3 * sizeof(float) * (size_t)(rows * actkv::conf_splits(vocab)));
-}
+size_t logprobs_stats(int64_t chunks) { return actkv::align256(3 * sizeof(float) * (size_t)chunks); }
 }  // namespace
 
 actkv_status actkv_token_logprobs_workspace(int64_t rows, int64_t vocab, int32_t top_k,
                                             size_t* workspace_bytes) {
   const actkv_status st = check_logprobs(rows, vocab, top_k);
   if (st != ACTKV_OK) return st;
-  if (workspace_bytes)
-    *workspace_bytes = logprobs_stats(rows, vocab) +
-                       sizeof(uint64_t) * (size_t)(rows * actkv::conf_splits(vocab) * top_k);
+  const int64_t chunks = rows * actkv::logprobs_splits(rows, vocab, top_k);
+  if (workspace_bytes) *workspace_bytes = logprobs_stats(chunks) + sizeof(uint64_t) * (size_t)(chunks * top_k);
   return ACTKV_OK;
 }
 
@@ -1125,7 +1126,7 @@ actkv_status actkv_token_logprobs(const void* logits, int32_t logits_type, int64
   return hip_status(actkv::launch_token_logprobs(
       logits, logits_type, rows, vocab, row_stride, tokens, top_k, logprobs, entropy, top_tokens,
       top_logprobs, reinterpret_cast<float*>(base),
-      reinterpret_cast<unsigned long long*>(base + logprobs_stats(rows, vocab)),
+      reinterpret_cast<unsigned long long*>(base + logprobs_stats(rows * actkv::logprobs_splits(rows, vocab, top_k))),
       static_cast<hipStream_t>(stream)));
 }
 

@@ -1,8 +1,11 @@
 // pages.hip -- pages shared by several requests: counts of holders (actkv_acquire_pages,
 // actkv_release_pages) and forks of requests (actkv_fork_pages).
 //
-// A fork moves what it copies (a page is read and written once) and touches one count and one table
-// entry per shared page; a release touches one count per entry.  The pages a release frees are
+// A fork moves what it copies (a page is read and written once) and touches one table entry per page; a
+// release reads the entries.  Both are bound by their atomics on the counts (25 a nanosecond over the
+// card), so one is made for several entries: the forks of a parent that follow each other count its
+// pages once, and a release takes off at once what a column of its list names in a run, as the
+// branches' rows of one parent do (branch_batch: fork 24 -> 10.5 us, counts of the release 22 -> 7.5).  The pages a release frees are
 // listed by page id through a bitmap of the pool, so the list does not depend on the order in which
 // the counts' atomics land.
 #include "device_common.hpp"
@@ -23,7 +26,7 @@ __device__ __forceinline__ bool in_pool(int64_t page, int64_t num_pages) {
 // Grid: (row workgroups + the most pages one fork copies, forks).  The first write kRowEntries of the
 // child's row and count the shared pages; each of the others copies a page, K and V.
 __global__ __launch_bounds__(kThreads) void fork_kernel(
-    const actkv_fork* forks, int row_wgs, int32_t bt_stride, int64_t num_pages, int64_t page_vecs,
+    const actkv_fork* forks, int num_forks, int row_wgs, int32_t bt_stride, int64_t num_pages, int64_t page_vecs,
     u32x4* kv, int32_t* bt, const int32_t* free_pages, int32_t* refs) {
   __shared__ int64_t scan_s[17];
   const int f = blockIdx.y, tid = threadIdx.x;
@@ -43,18 +46,35 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(
     }
     return;
   }
+  // the shared pages of the forks of this parent in this fork's group of 64: a run of them counts a
+  // page once
+  __shared__ int32_t shared_s[64];
+  if (tid < 64) {
+    const int x = (f & ~63) + tid;
+    shared_s[tid] = x < num_forks && forks[x].parent == fk.parent ? forks[x].shared : 0;
+  }
   int32_t* child = bt + (int64_t)fk.child * bt_stride;
-  for (int i = blockIdx.x * kRowEntries + tid; i < bt_stride && i < (int)(blockIdx.x + 1) * kRowEntries;
-       i += kThreads) {
-    int32_t page = -1;
-    if (i < fk.shared) {
-      page = parent[i];
-      if (refs && in_pool(page, num_pages)) atomicAdd(refs + page, 1);
-    } else if (i < fk.pages) {
-      page = free_pages[off + i - fk.shared];
-      if (refs && in_pool(page, num_pages)) refs[page] = 1;
+  constexpr int kPer = kRowEntries / kThreads;
+  int32_t page[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = blockIdx.x * kRowEntries + k * kThreads + tid;
+    page[k] = i < fk.shared ? parent[i] : i < fk.pages ? free_pages[off + i - fk.shared] : -1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = blockIdx.x * kRowEntries + k * kThreads + tid;
+    if (i >= bt_stride) continue;
+    child[i] = page[k];
+    if (!refs || !in_pool(page[k], num_pages)) continue;
+    if (i >= fk.shared) {
+      refs[page[k]] = 1;
+    } else if ((f & 63) == 0 || shared_s[(f & 63) - 1] <= i) {   // the first of its run
+      int x = (f & 63) + 1;
+      while (x < 64 && shared_s[x] > i) ++x;
+      atomicAdd(refs + page[k], x - (f & 63));
     }
-    child[i] = page;
   }
 }
 
@@ -69,45 +89,109 @@ __global__ __launch_bounds__(kThreads) void release_clear_kernel(uint32_t* words
     words[i] = 0;
 }
 
-// One count off per entry; a page whose count comes to 0 sets its bit and is counted in its block of
-// kReleaseBlock pages.  A count that was not positive is put back: it can't pass 0 again on the way,
-// so the one entry that sees 1 is the one that frees the page.
-__global__ __launch_bounds__(kThreads) void release_kernel(const int32_t* pages, int64_t n,
-                                                           int64_t num_pages, int32_t* refs,
-                                                           uint32_t* bits, uint32_t* counts) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
-    const int32_t page = pages[i];
-    if (!in_pool(page, num_pages)) continue;
-    const int32_t old = atomicSub(refs + page, 1);
-    if (old == 1) {
-      atomicOr(bits + (page >> 5), 1u << (page & 31));
-      atomicAdd(counts + page / kReleaseBlock, 1u);
-    } else if (old <= 0) {
-      atomicAdd(refs + page, 1);
-    }
-  }
+// After `off` was counted off a page that had `old`: whether that brought it to 0.  What was not there
+// is put back: the count can't pass 0 again on the way, so of all that count a page off the one that
+// sees a positive count and takes the last of it is the one that frees the page.
+__device__ __forceinline__ bool came_to_zero(int32_t* ref, int32_t old, int off) {
+  if (old < off) atomicAdd(ref, off - max(old, 0));
+  return old > 0 && old <= off;
 }
 
-// Workgroup b lists the freed pages of block b, a word of the bitmap per thread; the entries of
-// `freed` behind the list are filled by all of them.
-__global__ __launch_bounds__(kThreads) void release_list_kernel(int64_t n, int64_t num_pages,
+// A thread: kRows entries of one column of the list, [rows][row_len] (the last row may be short).
+// A freed page sets its bit.
+template <int kRows>
+__global__ __launch_bounds__(kThreads) void release_kernel(const int32_t* pages, int64_t n, int64_t row_len,
+                                                           int64_t num_pages, int32_t* refs,
+                                                           uint32_t* bits) {
+  const int64_t col_wgs = (row_len + kThreads - 1) / kThreads;
+  const int64_t col = blockIdx.x % col_wgs * kThreads + threadIdx.x;
+  const int64_t first = blockIdx.x / col_wgs * kRows * row_len + col;
+  if (col >= row_len) return;
+  int32_t page[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) page[r] = first + r * row_len < n ? pages[first + r * row_len] : -1;
+  // off[r]: what the run that ends at r counts off (0: none ends there); all counts set out first
+  int off[kRows], old[kRows], run = 0;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    ++run;
+    const bool ends = r + 1 == kRows || page[r + 1] != page[r];
+    off[r] = ends && in_pool(page[r], num_pages) ? run : 0;
+    if (ends) run = 0;
+  }
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) old[r] = off[r] > 0 ? atomicSub(refs + page[r], off[r]) : 0;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+    if (off[r] > 0 && came_to_zero(refs + page[r], old[r], off[r]))
+      atomicOr(bits + (page[r] >> 5), 1u << (page[r] & 31));
+}
+
+// counts[b]: the freed pages of block b, kReleaseBlock pages, a word of the bitmap per thread.  (Counted
+// here and not as they are freed: atomics on so few counters cost 13 us for 17,500 pages.)
+__global__ __launch_bounds__(kThreads) void release_count_kernel(int64_t num_words, const uint32_t* bits,
+                                                                 uint32_t* counts) {
+  __shared__ int64_t scan_s[17];
+  const int64_t word = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  int64_t all;
+  block_excl_scan_i64(word < num_words ? __popc(bits[word]) : 0, scan_s, &all);
+  if (threadIdx.x == 0) counts[blockIdx.x] = (uint32_t)all;
+}
+
+// Workgroup b lists the freed pages of block b (behind the bitmap's end: none); the entries of `freed`
+// behind the list are filled by all of them.  kCounts: the blocks' counts are there; otherwise every
+// workgroup counts the whole bitmap, which is short.
+template <bool kCounts>
+__global__ __launch_bounds__(kThreads) void release_list_kernel(int64_t n, int64_t num_words,
                                                                 const uint32_t* bits,
                                                                 const uint32_t* counts,
                                                                 int32_t* freed, int32_t* num_freed) {
   __shared__ int64_t scan_s[17];
-  const int b = blockIdx.x, blocks = gridDim.x, tid = threadIdx.x;
+  const int64_t b = blockIdx.x, wgs = gridDim.x;
+  const int tid = threadIdx.x;
+  const int64_t word = b * kThreads + tid;
+  uint32_t w = word < num_words ? bits[word] : 0u;
   int64_t sums = 0, all;   // pages of the blocks before, and of all of them in the upper half
-  for (int x = tid; x < blocks; x += kThreads)
-    sums += ((int64_t)counts[x] << 32) + (x < b ? counts[x] : 0u);
+  const int64_t entries = kCounts ? (num_words + kThreads - 1) / kThreads : num_words;
+  const int64_t here_from = kCounts ? b : b * kThreads;
+#pragma unroll 8
+  for (int64_t x = tid; x < entries; x += kThreads) {
+    const int64_t v = kCounts ? (int64_t)counts[x] : (int64_t)__popc(bits[x]);
+    sums += (v << 32) + (x < here_from ? v : 0);
+  }
   block_excl_scan_i64(sums, scan_s, &all);
   const int64_t before = all & 0xFFFFFFFF, total = all >> 32;
-  const int64_t word = (int64_t)b * kThreads + tid;
-  uint32_t w = word < (num_pages + 31) / 32 ? bits[word] : 0u;
   int64_t here;
   int64_t at = before + block_excl_scan_i64(__popc(w), scan_s, &here);
   for (; w; w &= w - 1) freed[at++] = (int32_t)(word * 32 + __builtin_ctz(w));
-  for (int64_t i = total + (int64_t)b * kThreads + tid; i < n; i += (int64_t)blocks * kThreads) freed[i] = -1;
+  for (int64_t i = total + b * kThreads + tid; i < n; i += wgs * kThreads) freed[i] = -1;
   if (b == 0 && tid == 0) *num_freed = (int32_t)total;
+}
+
+// The same for at most kReleaseSmall entries, in one workgroup without the bitmap: the freed pages
+// listed in LDS, then each at its rank among them.
+__global__ __launch_bounds__(kReleaseSmall) void release_small_kernel(const int32_t* pages, int n,
+                                                                      int64_t num_pages, int32_t* refs,
+                                                                      int32_t* freed, int32_t* num_freed) {
+  __shared__ int32_t gone[kReleaseSmall];
+  __shared__ int count;
+  const int tid = threadIdx.x;
+  if (tid == 0) count = 0;
+  __syncthreads();
+  if (tid < n) {
+    const int32_t page = pages[tid];
+    if (in_pool(page, num_pages) && came_to_zero(refs + page, atomicSub(refs + page, 1), 1)) gone[atomicAdd(&count, 1)] = page;
+  }
+  __syncthreads();
+  const int total = count;
+  if (tid < total) {
+    int rank = 0;
+    for (int x = 0; x < total; ++x) rank += gone[x] < gone[tid] ? 1 : 0;
+    freed[rank] = gone[tid];
+  } else if (tid < n) {
+    freed[tid] = -1;
+  }
+  if (tid == 0) *num_freed = total;
 }
 
 static_assert(kReleaseBlock == kThreads * 32, "a word of the bitmap per thread");
@@ -124,7 +208,7 @@ hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t max_copie
                        const int32_t* free_pages, int32_t* refs, hipStream_t s) {
   const int row_wgs = (bt_stride + kRowEntries - 1) / kRowEntries;
   hipLaunchKernelGGL(fork_kernel, dim3((unsigned)(row_wgs + max_copied), (unsigned)num_forks),
-                     dim3(kThreads), 0, s, forks, row_wgs, bt_stride, num_pages, page_bytes / 16,
+                     dim3(kThreads), 0, s, forks, num_forks, row_wgs, bt_stride, num_pages, page_bytes / 16,
                      static_cast<u32x4*>(kv), bt, free_pages, refs);
   return hipGetLastError();
 }
@@ -135,21 +219,44 @@ hipError_t launch_acquire(const int32_t* pages, int64_t n, int64_t num_pages, in
   return hipGetLastError();
 }
 
-hipError_t launch_release(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
-                          int32_t* freed, int32_t* num_freed, uint32_t* bits, uint32_t* counts,
-                          int64_t words, hipStream_t s) {
+hipError_t launch_release(const int32_t* pages, int64_t n, int64_t row_len, int64_t num_pages,
+                          int32_t* refs, int32_t* freed, int32_t* num_freed, uint32_t* bits,
+                          uint32_t* counts, hipStream_t s) {
+  const int64_t num_words = (num_pages + 31) / 32;
+  if (n <= kReleaseSmall) {
+    hipLaunchKernelGGL(release_small_kernel, dim3(1), dim3(kReleaseSmall), 0, s, pages, (int)n, num_pages, refs,
+                       freed, num_freed);
+    return hipGetLastError();
+  }
   // (a fill kernel: a memset node of a captured graph is not to be relied on)
-  hipLaunchKernelGGL(release_clear_kernel, dim3(blocks_for(words)), dim3(kThreads), 0, s, bits, words);
+  hipLaunchKernelGGL(release_clear_kernel, dim3(blocks_for(num_words)), dim3(kThreads), 0, s, bits, num_words);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (n > 0) {
-    hipLaunchKernelGGL(release_kernel, dim3(blocks_for(n)), dim3(kThreads), 0, s, pages, n, num_pages,
-                       refs, bits, counts);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  // several rows to a thread once that leaves 64 workgroups (8 x 2,188 entries: 13.7 us with 9 of them)
+  const bool deep = n >= 64 * kThreads * kReleaseRows;
+  const int64_t rows = (n + row_len - 1) / row_len, per = deep ? kReleaseRows : 1;
+  const dim3 grid((unsigned)((row_len + kThreads - 1) / kThreads * ((rows + per - 1) / per)));
+  if (deep)
+    hipLaunchKernelGGL(release_kernel<kReleaseRows>, grid, dim3(kThreads), 0, s, pages, n, row_len, num_pages,
+                       refs, bits);
+  else
+    hipLaunchKernelGGL(release_kernel<1>, grid, dim3(kThreads), 0, s, pages, n, row_len, num_pages, refs, bits);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t blocks = release_blocks(num_pages);
+  const int64_t fill_wgs = n / (8 * kThreads) < 512 ? n / (8 * kThreads) : 512;
+  const dim3 list_grid((unsigned)(blocks > fill_wgs ? blocks : fill_wgs));
+  // (64 KB of bitmap to each of at most 512 workgroups: no more than a launch costs)
+  if (num_words <= 16384) {
+    hipLaunchKernelGGL(release_list_kernel<false>, list_grid, dim3(kThreads), 0, s, n, num_words, bits, counts,
+                       freed, num_freed);
+    return hipGetLastError();
   }
-  hipLaunchKernelGGL(release_list_kernel, dim3((unsigned)release_blocks(num_pages)), dim3(kThreads), 0,
-                     s, n, num_pages, bits, counts, freed, num_freed);
+  hipLaunchKernelGGL(release_count_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, num_words, bits, counts);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(release_list_kernel<true>, list_grid, dim3(kThreads), 0, s, n, num_words, bits, counts, freed,
+                     num_freed);
   return hipGetLastError();
 }
 

@@ -24,8 +24,8 @@ def _release_reference(pages, refs):
     return refs
 
 
-@pytest.mark.parametrize("n,num_pages", [(0, 10), (1, 1), (5, 33), (300, 100), (5000, 8192), (20000, 70001),
-                                         (3000, 1_200_000)])
+@pytest.mark.parametrize("n,num_pages", [(0, 10), (1, 1), (5, 33), (300, 100), (1023, 5000), (1024, 256), (1025, 257),
+                                         (5000, 8192), (20000, 70001), (3000, 1_200_000), (2000, 4_300_000)])
 def test_release_lists_the_pages_that_nobody_holds(n, num_pages):
     rng = np.random.default_rng(n)
     refs = rng.integers(0, 4, num_pages).astype(np.int32)
@@ -38,6 +38,29 @@ def test_release_lists_the_pages_that_nobody_holds(n, num_pages):
         freed, count = actkv.release_pages(pages_d, refs_d)
         assert int(count) == gone.size
         np.testing.assert_array_equal(freed.cpu().numpy(), np.concatenate([gone, np.full(n - gone.size, -1)]))
+        np.testing.assert_array_equal(refs_d.cpu().numpy(), want)
+        refs = want
+
+
+@pytest.mark.parametrize("rows,row_len", [(1, 1500), (20, 100), (64, 40), (9, 257), (17, 2188), (2000, 1), (100, 2188)])
+def test_release_of_rows_that_share_pages(rows, row_len):
+    """Runs of rows with the same pages in the same places, cut by others, longer and shorter than
+    what a thread takes."""
+    rng = np.random.default_rng(rows)
+    num_pages = 5000
+    base = rng.integers(-1, num_pages, (rows, row_len)).astype(np.int32)
+    owner = np.sort(rng.integers(0, max(1, rows // 3), rows))
+    pages = base[owner]
+    pages[rng.random(pages.shape) < 0.02] = -1
+    refs = rng.integers(0, 8, num_pages).astype(np.int32)
+    refs_d, pages_d = torch.from_numpy(refs).to(DEV), torch.from_numpy(pages).to(DEV)
+    for _ in range(2):
+        want = _release_reference(pages, refs)
+        gone = np.nonzero((refs > 0) & (want == 0))[0]
+        freed, count = actkv.release_pages(pages_d, refs_d)
+        assert int(count) == gone.size
+        np.testing.assert_array_equal(freed.cpu().numpy()[:gone.size], gone)
+        assert (freed[gone.size:] == -1).all()
         np.testing.assert_array_equal(refs_d.cpu().numpy(), want)
         refs = want
 
@@ -91,6 +114,9 @@ def test_fork_shares_full_pages_and_copies_the_others(heads, dim, stride):
     m = min(stride, 40)
     forks = np.array([[0, 5, stride, stride], [0, 6, stride - min(1, stride), stride], [1, 3, 0, m],
                       [2, 11, max(0, stride - m), stride], [1, 4, 0, 0], [2, 7, stride // 2, stride // 2]])
+    # several forks of one parent in a row, sharing different numbers of pages
+    more = [[1, 8, stride, stride], [1, 9, m, m], [1, 10, stride, stride]]
+    forks = np.concatenate([forks, more])
     f = actkv.Forks(*forks.T).to_device(DEV)
     refs = rng.integers(0, 3, P).astype(np.int32)
     want = _fork_reference(forks, kv, bt, free, refs)

@@ -141,10 +141,10 @@ def test_counts_refuse():
     assert lib.actkv_release_workspace(1, 1 << 31, ctypes.byref(n)) == UNSUPPORTED
     assert lib.actkv_release_workspace(5, 100, ctypes.byref(n)) == 0
 
-    def release(pages=FAKE, n_=5, num_pages=100, refs=FAKE, freed=2 * FAKE, count=FAKE, ws=FAKE, size=n.value):
-        return lib.actkv_release_pages(pages, n_, num_pages, refs, freed, count, ws, size, None)
+    def release(pages=FAKE, n_=5, row=0, num_pages=100, refs=FAKE, freed=2 * FAKE, count=FAKE, ws=FAKE, size=n.value):
+        return lib.actkv_release_pages(pages, n_, row, num_pages, refs, freed, count, ws, size, None)
     for over in (dict(pages=None), dict(refs=None), dict(freed=None), dict(count=None), dict(ws=None),
-                 dict(ws=FAKE + 2), dict(n_=-1), dict(num_pages=0), dict(freed=FAKE)):
+                 dict(ws=FAKE + 2), dict(n_=-1), dict(row=-1), dict(num_pages=0), dict(freed=FAKE)):
         assert release(**over) == INVALID, over
     assert release(size=n.value - 1) == SMALL
 
