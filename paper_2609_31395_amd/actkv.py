@@ -8,6 +8,7 @@ this module without it raises, and there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from dataclasses import dataclass
@@ -833,15 +834,17 @@ class _Launch:
     stream is the caller's or that device's current one.  A buffer that the call makes for itself
     (`scratch`) belongs to the stream it runs on, so that its memory is not handed out again while
     the kernels run; one that the caller gets (`result`) is marked as in use there."""
-    __slots__ = ("device", "given", "handle", "_before")
+    __slots__ = ("like", "given", "handle", "_before")
 
-    def __init__(self, device: torch.device, stream):
-        self.device, self.given = device, stream
+    def __init__(self, like: torch.Tensor, stream):
+        self.like, self.given = like, stream   # like: a tensor of the call
 
     def __enter__(self):
-        self._before = torch._C._cuda_getDevice()
-        if self._before != self.device.index:
-            torch.cuda.set_device(self.device)
+        index = self.like.get_device()
+        self._before = -1
+        if torch._C._cuda_getDevice() != index:
+            self._before = torch._C._cuda_getDevice()
+            torch.cuda.set_device(index)
         try:
             self.handle = _stream(self.given)
         except BaseException:
@@ -850,21 +853,21 @@ class _Launch:
         return self
 
     def __exit__(self, *exc):
-        if self._before != self.device.index:
+        if self._before >= 0:
             torch.cuda.set_device(self._before)
 
     def _torch_stream(self):
         return (self.given if isinstance(self.given, torch.cuda.Stream)
-                else torch.cuda.ExternalStream(self.handle, device=self.device))
+                else torch.cuda.ExternalStream(self.handle, device=self.like.device))
 
     def scratch(self, size: int) -> torch.Tensor:
         if self.given is None:
-            return torch.empty(max(size, 1), dtype=torch.uint8, device=self.device)
+            return self.like.new_empty(size if size > 0 else 1, dtype=torch.uint8)
         with torch.cuda.stream(self._torch_stream()):
-            return torch.empty(max(size, 1), dtype=torch.uint8, device=self.device)
+            return self.like.new_empty(size if size > 0 else 1, dtype=torch.uint8)
 
     def result(self, shape, dtype) -> torch.Tensor:
-        t = torch.empty(shape, dtype=dtype, device=self.device)
+        t = self.like.new_empty(shape, dtype=dtype)
         if self.given is not None and t.numel() > 0:
             t.record_stream(self._torch_stream())
         return t
@@ -932,7 +935,7 @@ def attend(p: Problem, q: torch.Tensor, kv_cache: torch.Tensor, block_table: tor
         if _ws_bytes(ws) < need:
             raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
     _on_gpu(z.seen + z.mirrors)
-    with _Launch(kv_cache.device, stream) as on:
+    with _Launch(q, stream) as on:
         if out is None:
             out = on.result((z.sum_n, p.num_q_heads, p.head_dim), torch.bfloat16)
         if lse is None:
@@ -999,7 +1002,7 @@ def fork_pages(forks: Forks, kv_cache: torch.Tensor, block_table: torch.Tensor,
     if refs is not None and refs.numel() != pages:
         raise ValueError(f"refs holds {refs.numel()} counts, the cache {pages} pages")
     _on_gpu(seen)
-    with _Launch(block_table.device, stream) as on:
+    with _Launch(block_table, stream) as on:
         _check("actkv_fork_pages", lib.actkv_fork_pages(
             forks.host.ctypes.data, _ptr(forks.device), n, int(block_table.shape[0]),
             int(block_table.shape[1]), heads, dim, page, pages, _ptr(kv_cache), _ptr(block_table),
@@ -1016,22 +1019,18 @@ def acquire_pages(pages: torch.Tensor, refs: torch.Tensor, stream=None) -> torch
     if pages is None:
         raise ValueError("pages is required")
     _on_gpu(seen)
-    with _Launch(refs.device, stream) as on:
+    with _Launch(refs, stream) as on:
         _check("actkv_acquire_pages", lib.actkv_acquire_pages(
             _ptr(pages), pages.numel(), refs.numel(), _ptr(refs), on.handle))
     return refs
 
 
-_RELEASE_WS: dict = {}   # pool pages -> workspace bytes
-
-
+@functools.lru_cache(maxsize=1024)
 def _release_ws(num_pages: int) -> int:
-    if num_pages not in _RELEASE_WS:
-        need = ctypes.c_size_t()
-        _check("actkv_release_workspace",
-               load_library().actkv_release_workspace(0, num_pages, ctypes.byref(need)))
-        _RELEASE_WS[num_pages] = need.value
-    return _RELEASE_WS[num_pages]
+    need = ctypes.c_size_t()
+    _check("actkv_release_workspace",
+           load_library().actkv_release_workspace(0, num_pages, ctypes.byref(need)))
+    return need.value
 
 
 def release_workspace(num_pages: int, n: int, device="cuda") -> torch.Tensor:
@@ -1060,7 +1059,7 @@ def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch
         if _ws_bytes(ws) < need:
             raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
     _on_gpu(seen)
-    with _Launch(refs.device, stream) as on:
+    with _Launch(refs, stream) as on:
         if freed is None:
             freed = on.result((n,), torch.int32)
         if num_freed is None:
@@ -1070,6 +1069,14 @@ def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch
             _ptr(pages), n, int(pages.shape[-1]) if pages.dim() > 1 else 0, refs.numel(), _ptr(refs),
             _ptr(freed), _ptr(num_freed), _ptr(ws), _ws_bytes(ws), on.handle))
     return freed, num_freed
+
+
+@functools.lru_cache(maxsize=1024)
+def _logprobs_ws(rows: int, vocab: int, top_k: int) -> int:
+    need = ctypes.c_size_t()
+    _check("actkv_token_logprobs_workspace", load_library().actkv_token_logprobs_workspace(
+        rows, vocab, top_k, ctypes.byref(need)))
+    return need.value
 
 
 _LOGITS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -1102,15 +1109,13 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     _need("entropy", entropy, _F32, rows, required=False, seen=seen)
     _need("top_tokens", top_tokens, (torch.int64,), rows * top_k, required=False, seen=seen)
     _need("top_logprobs", top_logprobs, _F32, rows * top_k, required=False, seen=seen)
-    need = ctypes.c_size_t()
-    _check("actkv_token_logprobs_workspace", lib.actkv_token_logprobs_workspace(
-        rows, vocab, top_k, ctypes.byref(need)))
+    need = _logprobs_ws(rows, vocab, top_k)
     if ws is not None:
         _need("ws", ws, None, 0, seen=seen)
-        if _ws_bytes(ws) < need.value:
-            raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need.value}")
+        if _ws_bytes(ws) < need:
+            raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
     _on_gpu(seen)
-    with _Launch(logits.device, stream) as on:
+    with _Launch(logits, stream) as on:
         if logprobs is None and tokens is not None:
             logprobs = on.result((rows,), torch.float32)
         if entropy is None:
@@ -1122,7 +1127,7 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
                 top_logprobs = on.result((rows, top_k), torch.float32)
         else:
             top_tokens = top_logprobs = None
-        ws = on.scratch(need.value) if ws is None else ws
+        ws = on.scratch(need) if ws is None else ws
         _check("actkv_token_logprobs", lib.actkv_token_logprobs(
             _ptr(logits), _LOGITS[logits.dtype], rows, vocab,
             int(logits.stride(0)) if rows > 1 else vocab, _ptr(tokens), top_k, _ptr(logprobs),

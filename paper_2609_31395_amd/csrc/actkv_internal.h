@@ -303,9 +303,35 @@ inline int attend_head_waves(int Hkv, int D, int64_t rows, int64_t entries) {
   }
   return best;
 }
+// Whether each (request, group of heads) is one workgroup's, and of how many heads (*heads): no plan and
+// no join then, but nothing splits a long request.  max_L, entries: the longest request's and all
+// requests' entries; per_head: the heads have lengths of their own (one head to a workgroup then);
+// split_heads: the heads of a workgroup otherwise.  By estimated times, us: 3 to start an item and 3.5
+// (64-element heads 1.4) a step of a wave, against 10 to plan and join, 3 an item, the partials'
+// traffic and the join of their rows; neither faster than the memory (with lengths per head, of which the
+// host knows the bounds alone, a fifth of them).  From 50 us of memory on the split form evens out what
+// the CUs do and costs little.  (100 problems of 1-128 requests of 64-64,000 entries, both ways:
+// geometric means 23.6 us direct, 18.3 split, 15.8 as chosen; e.g. 51 x 94-119 entries of 8 heads 9.7
+// against 18.2, 42 x 1,051 30 against 37, 8 x 2,400-2,800 with lengths per head 30 against 14.)
+inline bool attend_direct(int R, int Hkv, int D, int64_t rows, int64_t max_L, int64_t entries, bool per_head,
+                          int split_heads, int* heads) {
+  const int waves = attend_waves(D, rows);
+  int hw = 1;   // as few as leave one round of workgroups
+  while (!per_head && (int64_t)R * Hkv > (int64_t)hw * kAttendMaxWgs && 2 * hw <= waves && Hkv % (2 * hw) == 0) hw *= 2;
+  *heads = hw;
+  const double wgs = (double)R * Hkv / hw, items = (double)R * Hkv / split_heads;
+  const int64_t longest = (max_L + kAttendStep - 1) / kAttendStep;
+  const double memory = 4.0 * D * Hkv * (double)entries / 5.9e6 * (per_head ? 0.2 : 1.0);
+  const double partials = 2.0 * kAttendMaxWgs * split_heads * rows * (4 * D + 8) / 5.9e6;
+  const double turns = (D == 128 ? 3.5 : 1.4) * (double)((longest * hw + waves - 1) / waves);
+  const double direct = 3.0 * (wgs > kAttendMaxWgs ? wgs / kAttendMaxWgs : 1.0) + (turns > memory ? turns : memory);
+  const double join = 1.2e-3 * R * Hkv * (double)rows;
+  return memory < 50.0 && direct < 10.0 + 3.0 * items / kAttendMaxWgs + partials + join + memory;
+}
 struct AttendArgs {
   int32_t R, Hq, Hkv, G, D, bt_stride, causal, max_rows;   // max_rows: most n * G of a request
-  int32_t head_waves;                   // KV heads of a workgroup (chosen at launch)
+  int32_t head_waves;                   // KV heads of a workgroup
+  int32_t direct;                       // 1: a workgroup per item, 0: equal shares and a join
   int32_t Hkv_slots;                    // heads a partial of a workgroup holds: Hkv, with kv_lens 1
   int64_t num_pages, q_stride, new_stride;
   float alpha;                          // sm_scale * log2(e)

@@ -981,7 +981,10 @@ actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_strid
   a.seq_lens = p->seq_lens_d;
   a.kv_lens = kv_lens;
   a.Hkv_slots = kv_lens ? 1 : hp.Hkv;
-  a.head_waves = kv_lens ? 1 : ap.head_waves;
+  int heads = 1;
+  a.direct = actkv::attend_direct(hp.R, hp.Hkv, hp.D, ap.max_rows, hp.max_L, hp.sum_L, kv_lens != nullptr,
+                                    kv_lens ? 1 : ap.head_waves, &heads);
+  a.head_waves = a.direct ? heads : kv_lens ? 1 : ap.head_waves;
   a.k_new = static_cast<const uint16_t*>(k_new);
   a.v_new = static_cast<const uint16_t*>(v_new);
   a.new_stride = new_stride;

@@ -195,47 +195,77 @@ void attend_kernel(AttendArgs a) {
   const int b = blockIdx.x / groups;
   const int h_wave = a.kv_lens ? 0 : (int)(blockIdx.x % groups) * hw + w % hw, k_wave = w / hw;
 
-  // the plan: cost and new tokens before each item (every workgroup finds its own share)
+  // a.direct: workgroup b has item b, all of it, and there is nothing to join.  Otherwise the plan: cost
+  // and new tokens before each item (every workgroup finds its own share).
   const int fixed = item_cost(hw);
   auto cost_of = [&](const Item& i) { const int n_steps = i.steps(); return n_steps > 0 ? n_steps + fixed : 0; };
-  const int per = ceil_div(items, kThreads);
-  int64_t own = 0;
-  Item it = {0, 0, 0};   // this thread's (last) item
-  for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
-    it = item_of(a, x);
-    own += ((int64_t)cost_of(it) << 32) + (!a.kv_lens || x % a.Hkv == 0 ? it.n : 0);
-  }
-  int64_t all;
-  const int64_t before = block_excl_scan_i64(own, scan_s, &all);
-  const int total = (int)(all >> 32);
-  const Shares shares(total, gridDim.x / groups);
-  const int c0 = b < shares.wgs ? shares.begin(b) : 0, c1 = b < shares.wgs ? shares.begin(b + 1) : 0;
-  const int t_before = (int)(before >> 32);
-  const bool mine = c0 < c1 && t_before <= c0 && c0 < t_before + (int)(own >> 32);
-  if (mine || blockIdx.x == 0) {
-    int t = t_before, q = (int)before;
-    for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
-      if (per > 1) it = item_of(a, x);
-      const int h = a.kv_lens ? x % a.Hkv : 0, cost = cost_of(it);
-      if (blockIdx.x == 0) {
-        a.start[x] = t;
-        if (h == 0) a.q_off[a.kv_lens ? x / a.Hkv : x] = q;
-      }
-      if (mine && t <= c0 && c0 < t + cost) {
-        first_s[0] = x;
-        first_s[1] = t;
-        first_s[2] = h == 0 ? q : q - it.n;
-        first_s[3] = it.n;
-        first_s[4] = it.cached;
-        first_s[5] = it.fresh;
-      }
-      t += cost;
-      if (h == 0) q += it.n;
+  Item it = {0, 0, 0};
+  int c0 = 0, c1 = 1 << 30;
+  if (a.direct) {
+    const int r = a.kv_lens ? b / a.Hkv : b;
+    int64_t own = 0, all;
+    for (int x = tid; x < r; x += kThreads) own += a.q_lens[x];
+    it = item_of(a, b);
+    block_excl_scan_i64(own, scan_s, &all);
+    if (tid == 0) {
+      first_s[0] = b;
+      first_s[1] = -fixed;
+      first_s[2] = (int)all;
+      first_s[3] = it.n;
+      first_s[4] = it.cached;
+      first_s[5] = it.fresh;
     }
-    if (blockIdx.x == 0 && tid == 0) a.start[items] = total;
+    if (it.steps() == 0) {   // rows that see no entry, of every head of the workgroup
+      const int rows = it.n * a.G, heads = a.kv_lens ? 1 : hw, h0 = a.kv_lens ? b % a.Hkv : (int)(blockIdx.x % groups) * hw;
+      for (int y = tid; y < rows * heads * D; y += kThreads) {
+        const int row = y / D, m = row % rows, j = m / a.G;
+        const int64_t at = (all + j) * a.Hq + (h0 + row / rows) * a.G + (m - j * a.G);
+        a.out[at * D + y % D] = 0;
+        if (a.lse && y % D == 0) a.lse[at] = kNegInf;
+      }
+      return;
+    }
+    __syncthreads();
+  } else {
+    const int per = ceil_div(items, kThreads);
+    int64_t own = 0;
+    for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
+      it = item_of(a, x);
+      own += ((int64_t)cost_of(it) << 32) + (!a.kv_lens || x % a.Hkv == 0 ? it.n : 0);
+    }
+    int64_t all;
+    const int64_t before = block_excl_scan_i64(own, scan_s, &all);
+    const int total = (int)(all >> 32);
+    const Shares shares(total, gridDim.x / groups);
+    c0 = b < shares.wgs ? shares.begin(b) : 0;
+    c1 = b < shares.wgs ? shares.begin(b + 1) : 0;
+    const int t_before = (int)(before >> 32);
+    const bool mine = c0 < c1 && t_before <= c0 && c0 < t_before + (int)(own >> 32);
+    if (mine || blockIdx.x == 0) {
+      int t = t_before, q = (int)before;
+      for (int x = tid * per; x < items && x < (tid + 1) * per; ++x) {
+        if (per > 1) it = item_of(a, x);
+        const int h = a.kv_lens ? x % a.Hkv : 0, cost = cost_of(it);
+        if (blockIdx.x == 0) {
+          a.start[x] = t;
+          if (h == 0) a.q_off[a.kv_lens ? x / a.Hkv : x] = q;
+        }
+        if (mine && t <= c0 && c0 < t + cost) {
+          first_s[0] = x;
+          first_s[1] = t;
+          first_s[2] = h == 0 ? q : q - it.n;
+          first_s[3] = it.n;
+          first_s[4] = it.cached;
+          first_s[5] = it.fresh;
+        }
+        t += cost;
+        if (h == 0) q += it.n;
+      }
+      if (blockIdx.x == 0 && tid == 0) a.start[items] = total;
+    }
+    if (c0 >= c1) return;
+    __syncthreads();
   }
-  if (c0 >= c1) return;
-  __syncthreads();
   int x = __builtin_amdgcn_readfirstlane(first_s[0]);
   int start = __builtin_amdgcn_readfirstlane(first_s[1]);
   int q_off = __builtin_amdgcn_readfirstlane(first_s[2]);
@@ -519,7 +549,7 @@ void attend_kernel(AttendArgs a) {
     }
     start += cost_of(it);
     if (!a.kv_lens || h == a.Hkv - 1) q_off += n;
-    if (start >= c1) break;   // (there is cost left, so there is another item)
+    if (a.direct || start >= c1) break;   // (there is cost left, so there is another item)
     const Item next = item_of(a, ++x);
     it.n = __builtin_amdgcn_readfirstlane(next.n);
     it.cached = __builtin_amdgcn_readfirstlane(next.cached);
@@ -529,7 +559,7 @@ void attend_kernel(AttendArgs a) {
 
 // The pieces of a segment (request and KV head) that several workgroups hold, and the rows of an empty
 // one.  kWide: a workgroup per row, for long segments in many pieces; otherwise a wave per row
-// (attend_draft, 5,120 rows of 2 or 3 pieces: ... against 15.6 us).
+// (attend_draft, 5,120 rows of 2 or 3 pieces: 8 against 15.6 us).
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
 
 template <int D, bool kWide>
@@ -645,6 +675,7 @@ hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s) {
     const int64_t shared_steps = a.kv_lens ? steps * a.Hkv : steps;
     if (wgs > shared_steps) wgs = shared_steps;
     wgs = (wgs < 1 ? 1 : wgs) * groups;
+    if (a.direct) wgs = (int64_t)groups * (a.kv_lens ? a.R * a.Hkv : a.R);
     hipLaunchKernelGGL((attend_kernel<D, kTiles>), dim3((unsigned)wgs), dim3(Sh::kThreads), 0, s, a);
   };
   auto run_d = [&](auto d) {
@@ -658,7 +689,7 @@ hipError_t launch_attend(AttendArgs a, int64_t steps, hipStream_t s) {
   if (a.D == 128) run_d(std::integral_constant<int, 128>());
   else run_d(std::integral_constant<int, 64>());
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.direct) return e;
   // more than 16 pieces to a segment in the mean: a workgroup per row
   const int64_t gangs = a.kv_lens ? wgs : wgs / (a.Hkv / a.head_waves);
   const bool wide = gangs > 16 * (int64_t)(a.kv_lens ? a.R * a.Hkv : a.R);

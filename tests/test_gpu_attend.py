@@ -157,9 +157,43 @@ def test_split_over_the_length_and_joined(heads, lens):
     b.check(actkv.attend(b.p, b.q, b.kv, b.bt_d))
 
 
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("heads,tokens", [((32, 4, 128), [2, 1, 0, 3, 1]), ((12, 12, 64), [5, 1, 0, 33, 2]),
+                                          ((16, 2, 128), [8, 1, 0, 1, 8]), ((24, 3, 128), [5, 2, 0, 1, 1]),
+                                          ((64, 8, 64), [6, 1, 0, 1, 8])])
+def test_split_pieces_of_every_kind(heads, tokens, per_head, append):
+    """Long requests beside short and empty ones, in shares that begin and end inside them."""
+    Hq, H, D = heads
+    lens = [9001, 300, 77, 17005, 64]
+    rng = np.random.default_rng(4)
+    per = None
+    if per_head:
+        per = np.stack([rng.integers(min(t, m) if append else 0, m + 1, H) for m, t in zip(lens, tokens)])
+        per[1, 0], per[3, -1] = tokens[1] if append else 0, 17005
+    b = Batch(heads, lens, tokens, 47, per_head=per)
+    k = v = None
+    if append:
+        N = int(b.n.sum())
+        k = torch.randn(N, H, D, device=DEV, dtype=torch.bfloat16)
+        v = torch.randn(N, H, D, device=DEV, dtype=torch.bfloat16)
+    got = actkv.attend(b.p, b.q, b.kv, b.bt_d, kv_lens=b.lens_d if per_head else None, k_new=k, v_new=v)
+    if append:
+        off = 0
+        for r, n in enumerate(tokens):
+            for h in range(H):
+                t = np.arange(int(b.lens[r, h]) - n, int(b.lens[r, h]))
+                page = torch.from_numpy(b.bt[r, t // 16].astype(np.int64)).to(DEV)
+                slot = torch.from_numpy(t % 16).to(DEV)
+                assert torch.equal(b.kv[0, page, slot, h], k[off:off + n, h])
+                assert torch.equal(b.kv[1, page, slot, h], v[off:off + n, h])
+            off += n
+    b.check(got)
+
+
 @pytest.mark.parametrize("heads", [(32, 4, 128), (40, 2, 64)])
 def test_logits_that_keep_rising(heads):
-    b = Batch(heads, [3001, 64, 500], [1, 1, 1], 9, rising=True, sm_scale=0.7)
+    b = Batch(heads, [23001, 64, 500], [1, 1, 1], 9, rising=True, sm_scale=0.7)
     b.check(actkv.attend(b.p, b.q, b.kv, b.bt_d))
 
 
@@ -196,9 +230,13 @@ def test_newest_tokens_are_written_first(heads, fused):
 
 
 def test_pages_outside_the_pool_read_as_zero_and_are_not_written():
-    b = Batch((8, 2, 64), [300, 20, 100], [1, 1, 2], 17)
+    for lens in ([300, 20, 100], [22300, 20, 100]):
+        _check_bad_pages(Batch((8, 2, 64), lens, [1, 1, 2], 17))
+
+
+def _check_bad_pages(b):
     bt = b.bt.copy()
-    bt[0, 3], bt[0, 18], bt[1, 1], bt[2, 6], bt[2, 0] = -1, b.kv.shape[1], 1 << 30, -7, -(1 << 31)
+    bt[0, 3], bt[0, b.bt.shape[1] - 1], bt[1, 1], bt[2, 6], bt[2, 0] = -1, b.kv.shape[1], 1 << 30, -7, -(1 << 31)
     bt_d = torch.from_numpy(bt).to(DEV)
     b.check(actkv.attend(b.p, b.q, b.kv, bt_d), bt=bt)
     before = b.kv.clone()
@@ -242,9 +280,10 @@ def test_outputs_beyond_the_batch_stay_and_the_lse_feeds_the_scoring():
         off += m
 
 
-def test_replayed_from_a_graph_with_lengths_that_grow():
+@pytest.mark.parametrize("longest", [500, 16370])
+def test_replayed_from_a_graph_with_lengths_that_grow(longest):
     """seq_lens are what the rows hold at most; the lengths are read on the device."""
-    b = Batch((32, 4, 128), [500, 60], [1, 1], 31, room=40)
+    b = Batch((32, 4, 128), [longest, 60], [1, 1], 31, room=40)
     k = torch.randn(2, 4, 128, device=DEV, dtype=torch.bfloat16)
     ws = actkv.attend_workspace(b.p)
     out = torch.empty(2, 32, 128, dtype=torch.bfloat16, device=DEV)

@@ -1,0 +1,167 @@
+"""The decode-step operators with the compression, as an engine runs them: requests are forked into
+branches over shared pages, every branch decodes a few tokens (attention with the new tokens' rows
+appended, its log-sum-exp into the streaming scores, the logits' monitors), one branch of each request is
+kept and compressed with unequal head budgets, the others are released, and decoding goes on with a
+length per head.  A dense copy of every branch's rows follows along; attention is checked as in
+test_gpu_attend, everything that is moved or counted exactly."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_31395_amd import actkv
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+HQ, H, D, WIDTH = 8, 2, 64, 64
+G = HQ // H
+
+
+class Engine:
+    def __init__(self, lens, rows, seed):
+        self.gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.num_pages = 400
+        self.kv = torch.full((2, self.num_pages, 16, H, D), math.nan, dtype=torch.bfloat16, device=DEV)
+        self.table = torch.full((rows, WIDTH), -1, dtype=torch.int32, device=DEV)
+        self.refs = torch.zeros(self.num_pages, dtype=torch.int32, device=DEV)
+        self.free = [int(p) for p in np.random.default_rng(seed).permutation(self.num_pages)]
+        self.lens = np.zeros((rows, H), np.int64)
+        self.dense = {}   # (row, head) -> [2, entries, D]
+        self.live = []
+        for r, m in enumerate(lens):
+            for p in range(-(-m // 16)):
+                self.grow(r, p)
+            for h in range(H):
+                x = self.randn(2, m, D)
+                t = torch.arange(m, device=DEV)
+                self.kv[:, self.table[r, t // 16].long(), t % 16, h] = x
+                self.dense[r, h] = x
+            self.lens[r] = m
+            self.live.append(r)
+
+    def randn(self, *shape):
+        return torch.randn(*shape, device=DEV, dtype=torch.bfloat16, generator=self.gen)
+
+    def take(self, n):
+        return torch.tensor([self.free.pop() for _ in range(n)], dtype=torch.int32, device=DEV)
+
+    def grow(self, r, p):
+        page = self.take(1)
+        self.table[r, p] = page[0]
+        actkv.acquire_pages(page, self.refs)
+
+    def problem(self, rows, tokens, budgets=None):
+        lens = self.lens[rows]
+        return actkv.Problem(seq_lens=lens.max(axis=1), q_lens=np.full(len(rows), tokens),
+                             budgets=np.zeros(lens.size) if budgets is None else budgets, num_q_heads=HQ,
+                             num_kv_heads=H, head_dim=D, num_pages=self.num_pages, bt_stride=WIDTH).to_device(DEV)
+
+    def check_counts(self):
+        want = np.zeros(self.num_pages, np.int64)
+        table = self.table.cpu().numpy()
+        for r in self.live:
+            held = table[r][table[r] >= 0]
+            want[held] += 1
+        np.testing.assert_array_equal(self.refs.cpu().numpy(), want)
+        assert not set(self.free) & set(np.nonzero(want)[0].tolist())
+        assert len(self.free) + int((want > 0).sum()) == self.num_pages
+
+    def decode(self, rows):
+        """One token for every row; returns its log-sum-exp and queries."""
+        for r in rows:
+            self.lens[r] += 1
+            if self.table[r, (self.lens[r].max() - 1) // 16] < 0:
+                self.grow(r, int(self.lens[r].max() - 1) // 16)
+        p = self.problem(rows, 1)
+        qkv = self.randn(len(rows), HQ + 2 * H, D)
+        q, k, v = qkv[:, :HQ], qkv[:, HQ:HQ + H], qkv[:, HQ + H:]
+        bt = self.table[torch.tensor(rows, device=DEV)]
+        kv_lens = torch.from_numpy(self.lens[rows].astype(np.int32).reshape(-1)).to(DEV)
+        out, lse = actkv.attend(p, q, self.kv, bt, kv_lens=kv_lens, k_new=k, v_new=v)
+        for i, r in enumerate(rows):
+            for h in range(H):
+                x = torch.stack((k[i, h], v[i, h]))[:, None]
+                self.dense[r, h] = torch.cat((self.dense[r, h], x), 1)
+                kk, vv = self.dense[r, h].double()
+                assert kk.shape[0] == self.lens[r, h]
+                qq = q[i, h * G:h * G + G].double()
+                logits = qq @ kk.T / math.sqrt(D)
+                prob = torch.softmax(logits, 1)
+                want = prob @ vv
+                d = (D + 16) * 2.0 ** -24 / math.sqrt(D) * (qq.abs() @ kk.abs().T).amax(1, keepdim=True)
+                tol = (2 * d + 2.0 ** -16) * (prob @ vv.abs()) + 2.0 ** -8 * want.abs()
+                assert ((out[i, h * G:h * G + G].double() - want).abs() <= tol).all(), (r, h)
+                want = torch.logsumexp(logits, 1)
+                assert ((lse[i, h * G:h * G + G].double() - want).abs()
+                        <= d[:, 0] + 2.0 ** -20 * (1 + want.abs())).all()
+        return p, q.contiguous(), bt, lse
+
+
+def test_branches_decode_are_compressed_and_go_on():
+    e = Engine([530, 131], 6, 3)
+    e.check_counts()
+    # two branches of each request beside it
+    forks = actkv.Forks.of_lengths([0, 0, 1, 1], [2, 3, 4, 5], e.lens[[0, 0, 1, 1]]).to_device(DEV)
+    fresh = e.take(forks.num_fresh)
+    actkv.fork_pages(forks, e.kv, e.table, fresh, e.refs)
+    for parent, child in zip(forks.parents, forks.children):
+        e.lens[child] = e.lens[parent]
+        for h in range(H):
+            e.dense[int(child), h] = e.dense[int(parent), h].clone()
+        e.live.append(int(child))
+    e.check_counts()
+    rows = sorted(e.live)
+    # each decodes 20 tokens of its own, past the shared pages and into new ones; their scores add up
+    acc = None
+    for step in range(20):
+        p, q, bt, lse = e.decode(rows)
+        if acc is None:
+            acc = torch.zeros(actkv.num_scores(p), device=DEV)
+        else:   # every segment grows by an entry
+            parts = acc.split([int(m) - 1 for m in p.seq_lens for _ in range(H)])
+            acc = torch.cat([torch.nn.functional.pad(x, (0, 1)) for x in parts])
+        actkv.score_accumulate(p, q, e.kv, bt, acc, lse=lse)
+    total = [float(x.double().sum()) for x in acc.split([int(m) for m in p.seq_lens for _ in range(H)])]
+    np.testing.assert_allclose(total, 20 * G, rtol=2e-3)   # each token's probabilities sum to one
+    e.check_counts()
+    # the branch to keep by the mean log probability of its tokens, beside the confidence monitor
+    logits = torch.randn(len(rows), 5000, device=DEV, generator=e.gen) * 3
+    r = actkv.token_logprobs(logits, logits.argmax(1), top_k=20)
+    assert torch.equal(r["logprobs"], r["top_logprobs"][:, 0]) and torch.equal(r["top_tokens"][:, 0], logits.argmax(1))
+    conf = actkv.token_confidence(logits, top_k=20)
+    assert ((conf + r["top_logprobs"].mean(1)).abs() <= 4e-5).all()
+    order = r["logprobs"].cpu().numpy()
+    keep = [max((r for r in rows if r % 6 in group), key=lambda r: order[rows.index(r)]) for group in ((0, 2, 3), (1, 4, 5))]
+    drop = [r for r in rows if r not in keep]
+    freed, count = actkv.release_pages(e.table[torch.tensor(drop, device=DEV)], e.refs)
+    e.free += freed[:int(count)].tolist()
+    e.table[torch.tensor(drop, device=DEV)] = -1
+    e.live = keep
+    e.check_counts()
+    # compressed with unequal budgets: fresh pages taken, the old ones given back
+    budgets = np.array([[200, 37], [16, 90]])
+    p = e.problem(keep, 1, budgets.reshape(-1))
+    scores = torch.cat([acc.split([int(m) for m in e.lens[rows].max(axis=1) for _ in range(H)])[rows.index(r) * H + h]
+                        for r in keep for h in range(H)])
+    qy = actkv.query(p)
+    fresh = e.take(qy["fresh_pages_needed"])
+    bt = e.table[torch.tensor(keep, device=DEV)].contiguous()
+    kept = torch.empty(qy["num_kept"], dtype=torch.int32, device=DEV)
+    res = actkv.select_compact(p, scores, e.kv, bt, fresh, kept=kept)
+    actkv.acquire_pages(fresh, e.refs)
+    freed, count = actkv.release_pages(res["freed"], e.refs)
+    e.free += freed[:int(count)].tolist()
+    e.table[torch.tensor(keep, device=DEV)] = bt
+    off = 0
+    for i, r in enumerate(keep):
+        for h in range(H):
+            n = int(budgets[i, h])
+            e.dense[r, h] = e.dense[r, h][:, kept[off:off + n].long()]
+            off += n
+        e.lens[r] = budgets[i]
+    np.testing.assert_array_equal(res["new_lens"].cpu().numpy().reshape(-1, H), budgets)
+    e.check_counts()
+    for _ in range(18):   # a length per head from here on
+        e.decode(keep)
+    e.check_counts()
