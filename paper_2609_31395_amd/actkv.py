@@ -278,6 +278,14 @@ def _need(name: str, t: Optional[torch.Tensor], dtypes, numel: int, required: bo
         seen.append((name, t))
 
 
+def _arg(seen: list, name: str, t, dtypes, numel: int, required: bool = True) -> None:
+    """_need with `seen`; an argument that is in order takes no further call."""
+    if type(t) is _TENSOR and t.dtype in dtypes and t.is_contiguous() and t.numel() >= numel:
+        seen.append((name, t))
+    elif t is not None or (required and numel > 0):
+        _need(name, t, dtypes, numel, required=required, seen=seen)
+
+
 def _on_gpu(named) -> None:
     """Every tensor resident on the same GPU."""
     if named and named[0][1].is_cuda:   # the usual case: one pass that finds nothing
@@ -992,13 +1000,13 @@ def fork_pages(forks: Forks, kv_cache: torch.Tensor, block_table: torch.Tensor,
     if not isinstance(kv_cache, torch.Tensor) or kv_cache.dim() != 5 or kv_cache.shape[0] != 2:
         raise ValueError("kv_cache must be [2, pages, page_size, kv heads, head dim]")
     _, pages, page, heads, dim = (int(x) for x in kv_cache.shape)
-    _need("kv_cache", kv_cache, _BITS16, 0, seen=seen)
+    _arg(seen, "kv_cache", kv_cache, _BITS16, 0)
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be [rows, stride]")
-    _need("block_table", block_table, _I32, 0, seen=seen)
-    _need("free_pages", free_pages, _I32, max(forks.num_fresh, 0), seen=seen)
-    _need("refs", refs, _I32, pages, required=False, seen=seen)
-    _need("forks", forks.device, _I32, 4 * n, seen=seen)
+    _arg(seen, "block_table", block_table, _I32, 0)
+    _arg(seen, "free_pages", free_pages, _I32, max(forks.num_fresh, 0))
+    _arg(seen, "refs", refs, _I32, pages, required=False)
+    _arg(seen, "forks", forks.device, _I32, 4 * n)
     if refs is not None and refs.numel() != pages:
         raise ValueError(f"refs holds {refs.numel()} counts, the cache {pages} pages")
     _on_gpu(seen)
@@ -1014,8 +1022,8 @@ def acquire_pages(pages: torch.Tensor, refs: torch.Tensor, stream=None) -> torch
     """refs[page] += 1 for every entry of pages (entries outside the pool are passed over)."""
     lib = load_library()
     seen: list = []
-    _need("pages", pages, _I32, 0, seen=seen)
-    _need("refs", refs, _I32, 1, seen=seen)
+    _arg(seen, "pages", pages, _I32, 0)
+    _arg(seen, "refs", refs, _I32, 1)
     if pages is None:
         raise ValueError("pages is required")
     _on_gpu(seen)
@@ -1048,11 +1056,11 @@ def release_pages(pages: torch.Tensor, refs: torch.Tensor, freed: Optional[torch
     seen: list = []
     if pages is None:
         raise ValueError("pages is required")
-    _need("pages", pages, _I32, 0, seen=seen)
+    _arg(seen, "pages", pages, _I32, 0)
     n = pages.numel()
-    _need("refs", refs, _I32, 1, seen=seen)
-    _need("freed", freed, _I32, n, required=False, seen=seen)
-    _need("num_freed", num_freed, _I32, 1, required=False, seen=seen)
+    _arg(seen, "refs", refs, _I32, 1)
+    _arg(seen, "freed", freed, _I32, n, required=False)
+    _arg(seen, "num_freed", num_freed, _I32, 1, required=False)
     need = _release_ws(refs.numel())
     if ws is not None:
         _need("ws", ws, None, 0, seen=seen)
@@ -1102,13 +1110,13 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
         raise ValueError("logits rows must not overlap")
     top_k = int(top_k)
     seen = [("logits", logits)]
-    _need("tokens", tokens, (torch.int64,), rows, required=False, seen=seen)
+    _arg(seen, "tokens", tokens, (torch.int64,), rows, required=False)
     if tokens is None and logprobs is not None:
         raise ValueError("logprobs needs tokens")
-    _need("logprobs", logprobs, _F32, rows, required=False, seen=seen)
-    _need("entropy", entropy, _F32, rows, required=False, seen=seen)
-    _need("top_tokens", top_tokens, (torch.int64,), rows * top_k, required=False, seen=seen)
-    _need("top_logprobs", top_logprobs, _F32, rows * top_k, required=False, seen=seen)
+    _arg(seen, "logprobs", logprobs, _F32, rows, required=False)
+    _arg(seen, "entropy", entropy, _F32, rows, required=False)
+    _arg(seen, "top_tokens", top_tokens, (torch.int64,), rows * top_k, required=False)
+    _arg(seen, "top_logprobs", top_logprobs, _F32, rows * top_k, required=False)
     need = _logprobs_ws(rows, vocab, top_k)
     if ws is not None:
         _need("ws", ws, None, 0, seen=seen)

@@ -919,7 +919,8 @@ actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   for (int r = 0; r < hp.R; ++r)
     ap->steps += (p->seq_lens_h[r] + (int64_t)actkv::kAttendStep - 1) / actkv::kAttendStep;
   const int64_t segs = (int64_t)hp.R * hp.Hkv;
-  if (ap->steps * hp.Hkv > INT32_MAX / 2 || segs > INT32_MAX / 2) return ACTKV_ERR_UNSUPPORTED;
+  // (2^22 segments: a grid's threads stay below 2^32)
+  if (ap->steps * hp.Hkv > INT32_MAX / 4 || segs > (1 << 22)) return ACTKV_ERR_UNSUPPORTED;
   // two partials per workgroup and head of it
   ap->head_waves = actkv::attend_head_waves(hp.Hkv, hp.D, ap->max_rows, hp.sum_L);
   int64_t slots = (int64_t)actkv::kAttendMaxWgs * ap->head_waves;
@@ -956,6 +957,7 @@ actkv_status actkv_attend(const actkv_problem* p, const void* q, int64_t q_strid
   if ((k_new == nullptr) != (v_new == nullptr)) return ACTKV_ERR_INVALID_ARGUMENT;
   if (q_stride < (int64_t)hp.Hq * hp.D || q_stride % 8) return ACTKV_ERR_INVALID_ARGUMENT;
   if (k_new && (new_stride < (int64_t)hp.Hkv * hp.D || new_stride % 8)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (k_new && new_stride > (1 << 26)) return ACTKV_ERR_UNSUPPORTED;   // 16 rows of it within 2 GB
   if (!aligned16(q) || !aligned16(kv_cache) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out) ||
       !aligned16(workspace))
     return ACTKV_ERR_INVALID_ARGUMENT;
@@ -1013,7 +1015,7 @@ namespace {
 actkv_status check_release(int64_t n, int64_t num_pages) {
   if (n < 0 || num_pages <= 0) return ACTKV_ERR_INVALID_ARGUMENT;
   // page ids and the number of freed pages are int32
-  if (num_pages > INT32_MAX || n > (INT64_C(1) << 36)) return ACTKV_ERR_UNSUPPORTED;
+  if (num_pages > INT32_MAX || n > INT32_MAX) return ACTKV_ERR_UNSUPPORTED;
   return ACTKV_OK;
 }
 int64_t release_words(int64_t num_pages) {
@@ -1057,7 +1059,7 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
       page_size <= 0 || num_pages <= 0 || num_free < 0)
     return ACTKV_ERR_INVALID_ARGUMENT;
   if ((head_dim != 64 && head_dim != 128) || page_size != actkv::kPageSize || num_kv_heads > 64 ||
-      num_forks > 65535)
+      num_forks > 65535 || bt_stride > (1 << 23))
     return ACTKV_ERR_UNSUPPORTED;
   if (num_forks == 0) return ACTKV_OK;
   if (!forks_h || !forks_d || !block_table) return ACTKV_ERR_INVALID_ARGUMENT;
@@ -1092,7 +1094,7 @@ actkv_status check_logprobs(int64_t rows, int64_t vocab, int32_t top_k) {
   if (rows < 0 || vocab < 1 || top_k < 0) return ACTKV_ERR_INVALID_ARGUMENT;
   if (top_k > actkv::kConfMaxTopK) return ACTKV_ERR_UNSUPPORTED;
   if (vocab > (int64_t)actkv::kConfMaxSplits * actkv::kConfChunkLogits) return ACTKV_ERR_UNSUPPORTED;
-  if (rows > INT32_MAX / actkv::kConfMaxSplits) return ACTKV_ERR_UNSUPPORTED;
+  if (rows > (1 << 20)) return ACTKV_ERR_UNSUPPORTED;   // a grid's threads stay below 2^32
   return ACTKV_OK;
 }
 size_t logprobs_stats(int64_t chunks) { return actkv::align256(3 * sizeof(float) * (size_t)chunks); }

@@ -43,7 +43,8 @@ def attend_bytes(p):
     (dict(q=FAKE + 8), INVALID), (dict(out=FAKE + 2), INVALID), (dict(kv=FAKE + 4), INVALID),
     (dict(ws=FAKE + 8), INVALID), (dict(k=FAKE), INVALID), (dict(v=FAKE), INVALID),
     (dict(k=FAKE, v=FAKE, stride=64), INVALID), (dict(k=FAKE, v=FAKE, stride=132), INVALID),
-    (dict(k=FAKE + 8, v=FAKE, stride=128), INVALID), (dict(ws_bytes=64), SMALL), (dict(mirrors=False), INVALID),
+    (dict(k=FAKE + 8, v=FAKE, stride=128), INVALID), (dict(k=FAKE, v=FAKE, stride=1 << 27), UNSUPPORTED),
+    (dict(ws_bytes=64), SMALL), (dict(mirrors=False), INVALID),
 ])
 def test_attend_refuses(over, code):
     assert c_attend(**over) == code
@@ -119,7 +120,7 @@ def c_fork(forks, rows=6, stride=4, **over):
     ([[0, 1, 1, 1]], dict(dim=96), UNSUPPORTED), ([[0, 1, 1, 1]], dict(page=32), UNSUPPORTED),
     ([[0, 1, 1, 1]], dict(heads=65), UNSUPPORTED), ([[0, 1, 1, 1]], dict(heads=0), INVALID),
     ([[0, 1, 1, 1]], dict(pages=0), INVALID), ([[0, 1, 1, 1]], dict(n=65536), UNSUPPORTED),
-    ([[0, 1, 1, 1]], dict(n=-1), INVALID), ([[0, 1, 1, 1]], dict(rows=-1), INVALID),
+    ([[0, 1, 1, 1]], dict(stride=1 << 24), UNSUPPORTED), ([[0, 1, 1, 1]], dict(n=-1), INVALID), ([[0, 1, 1, 1]], dict(rows=-1), INVALID),
 ])
 def test_fork_refuses(forks, over, code):
     assert c_fork(forks, **over) == code
@@ -139,6 +140,7 @@ def test_counts_refuse():
     n = ctypes.c_size_t()
     assert lib.actkv_release_workspace(-1, 8, ctypes.byref(n)) == INVALID
     assert lib.actkv_release_workspace(1, 1 << 31, ctypes.byref(n)) == UNSUPPORTED
+    assert lib.actkv_release_workspace(1 << 31, 100, ctypes.byref(n)) == UNSUPPORTED
     assert lib.actkv_release_workspace(5, 100, ctypes.byref(n)) == 0
 
     def release(pages=FAKE, n_=5, row=0, num_pages=100, refs=FAKE, freed=2 * FAKE, count=FAKE, ws=FAKE, size=n.value):
@@ -198,7 +200,7 @@ def c_logprobs(**over):
     (dict(x=None), INVALID), (dict(x=FAKE + 2), INVALID), (dict(x=FAKE + 1, type=1), INVALID), (dict(type=3), INVALID),
     (dict(type=-1), INVALID), (dict(rows=-1), INVALID), (dict(vocab=0), INVALID), (dict(stride=999), INVALID),
     (dict(tokens=None), INVALID), (dict(k=-1), INVALID), (dict(k=65), UNSUPPORTED), (dict(tt=None), INVALID),
-    (dict(tl=None), INVALID), (dict(vocab=262145, stride=262145), UNSUPPORTED), (dict(rows=1 << 28), UNSUPPORTED),
+    (dict(tl=None), INVALID), (dict(vocab=262145, stride=262145), UNSUPPORTED), (dict(rows=(1 << 20) + 1), UNSUPPORTED),
     (dict(ws=None), INVALID), (dict(ws=FAKE + 4), INVALID), (dict(size=8), SMALL),
 ])
 def test_logprobs_refuses(over, code):
