@@ -839,9 +839,9 @@ def check_pages(p: Problem, block_table: torch.Tensor, free_pages: Optional[torc
 
 class _Launch:
     """Where a call's kernels go: the device of its tensors is made current around it, and the
-    stream is the caller's or that device's current one.  A buffer that the call makes for itself
-    (`scratch`) belongs to the stream it runs on, so that its memory is not handed out again while
-    the kernels run; one that the caller gets (`result`) is marked as in use there."""
+    stream is the caller's or that device's current one.  What the call makes belongs to the stream it
+    runs on, so that neither an earlier holder of the memory nor a later one meets its kernels; a
+    `result`, which the caller gets, is marked as in use on the current stream as well."""
     __slots__ = ("like", "given", "handle", "_before")
 
     def __init__(self, like: torch.Tensor, stream):
@@ -875,9 +875,13 @@ class _Launch:
             return self.like.new_empty(size if size > 0 else 1, dtype=torch.uint8)
 
     def result(self, shape, dtype) -> torch.Tensor:
-        t = self.like.new_empty(shape, dtype=dtype)
-        if self.given is not None and t.numel() > 0:
-            t.record_stream(self._torch_stream())
+        if self.given is None:
+            return self.like.new_empty(shape, dtype=dtype)
+        current = torch.cuda.current_stream()
+        with torch.cuda.stream(self._torch_stream()):
+            t = self.like.new_empty(shape, dtype=dtype)
+        if current.cuda_stream != self.handle and t.numel() > 0:
+            t.record_stream(current)
         return t
 
 

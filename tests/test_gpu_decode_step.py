@@ -165,3 +165,27 @@ def test_branches_decode_are_compressed_and_go_on():
     for _ in range(18):   # a length per head from here on
         e.decode(keep)
     e.check_counts()
+
+
+def stream_of(t):
+    """The stream whose pool t's memory comes from."""
+    return next(s["stream"] for s in torch.cuda.memory_snapshot()
+                if s["address"] <= t.data_ptr() < s["address"] + s["total_size"])
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_what_a_call_makes_belongs_to_its_stream(raw):
+    """Memory that the current stream's work may still use is not written from another stream."""
+    e = Engine([40, 17], 2, 5)
+    p = e.problem([0, 1], 1)
+    q = e.randn(2, HQ, D)
+    logits = torch.randn(3, 100, device=DEV)
+    tokens = torch.zeros(3, dtype=torch.int64, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    s = side.cuda_stream if raw else side
+    got = [*actkv.attend(p, q, e.kv, e.table, stream=s), *actkv.release_pages(e.table, e.refs, stream=s),
+           *actkv.token_logprobs(logits, tokens, top_k=3, stream=s).values()]
+    torch.cuda.synchronize()
+    assert [stream_of(t) for t in got] == [side.cuda_stream] * len(got)
+    assert stream_of(actkv.attend(p, q, e.kv, e.table)[0]) == stream_of(q)
