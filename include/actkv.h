@@ -482,11 +482,12 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
  * of the result, whatever they hold.  Entries behind a page outside [0, num_pages) have K and V of
  * zero (their logit is 0).  q, K and V of the entries are finite.  Sums and the softmax are fp32; the
  * probabilities enter the second product as the sum of two bf16 values (16 bits).  At most
- * ACTKV_ATTEND_MAX_ROWS query rows per KV head and request (n_r * G), 2^22 (request, KV head) pairs and
- * a new_stride of 2^26: ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte aligned (lse and kv_lens: 4).
- * k_new, v_new, q, out and lse must not overlap the cache.  budgets are not used.  workspace: at least
- * the bytes that actkv_attend_workspace reports (host only, callable without a device).  No atomics:
- * results do not depend on scheduling.
+ * ACTKV_ATTEND_MAX_ROWS query rows per KV head and request (n_r * G), 2^30 entries of a request, 2^22
+ * (request, KV head) pairs and a new_stride of 2^26: ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte
+ * aligned (lse and kv_lens: 4).  k_new, v_new, q, out and lse must not overlap the cache, nor out and
+ * lse what the call reads.  budgets are not used.  workspace: at least the bytes that
+ * actkv_attend_workspace reports (host only, callable without a device).  No atomics: results do not
+ * depend on scheduling.
  */
 #define ACTKV_ATTEND_MAX_ROWS 64
 actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_bytes);
@@ -533,8 +534,8 @@ actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t row_le
  * entered in the row and neither written nor counted.  refs may be NULL (nothing shared between
  * live requests is counted).  forks_h: host array of num_forks, forks_d its device mirror.  Rows lie
  * in [0, num_rows); a child is nobody's parent and the child of one fork only, and pages <=
- * bt_stride (at most 2^23; at most 65,535 forks).  free_pages must not contain live pages; fewer than needed: ACTKV_ERR_OUT_OF_PAGES.
- * What a child's row held is overwritten (release it first).
+ * bt_stride (at most 2^23; at most 65,535 forks).  free_pages lists each page once and no live one;
+ * fewer than needed: ACTKV_ERR_OUT_OF_PAGES.  What a child's row held is overwritten (release it first).
  */
 typedef struct actkv_fork {
   int32_t parent, child, shared, pages;
@@ -560,8 +561,8 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
  * NULL.  A row whose every token is masked has log probabilities of -inf and an entropy of 0.  Rows
  * that hold +inf or NaN have unspecified values (never a fault; top_tokens stay within [-1, vocab)).
  * Sums are fp32 per chunk of the row in a fixed order, joined in fp64: results do not depend on
- * scheduling.  top_k in 0..64, vocab up to 262,144, rows up to 2^20 (else ACTKV_ERR_UNSUPPORTED).  workspace: at
- * least the bytes that actkv_token_logprobs_workspace reports.
+ * scheduling.  top_k in 0..64, vocab up to 262,144, rows up to 2^20 (else ACTKV_ERR_UNSUPPORTED).
+ * workspace: at least the bytes that actkv_token_logprobs_workspace reports.
  */
 typedef enum actkv_logits_type {
   ACTKV_LOGITS_F32 = 0,

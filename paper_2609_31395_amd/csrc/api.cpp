@@ -916,6 +916,8 @@ actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   const HostPlan& hp = ap->hp;
   ap->max_rows = hp.max_n * hp.G;
   if (ap->max_rows > ACTKV_ATTEND_MAX_ROWS) return ACTKV_ERR_UNSUPPORTED;
+  // (entry numbers are int32, those of the steps that are looked up ahead too)
+  if (hp.max_L > (1 << 30)) return ACTKV_ERR_UNSUPPORTED;
   for (int r = 0; r < hp.R; ++r)
     ap->steps += (p->seq_lens_h[r] + (int64_t)actkv::kAttendStep - 1) / actkv::kAttendStep;
   const int64_t segs = (int64_t)hp.R * hp.Hkv;

@@ -5,7 +5,8 @@
 // there are G (8, say) per new token.  So the work is split over the cache's length into equal
 // shares of 32-key steps, one per workgroup, whatever the lengths; each wave streams its steps of K
 // and V from global memory straight into MFMA operands, and the pieces of a (request, head) that
-// several workgroups hold are joined by a second kernel.
+// several workgroups hold are joined by a second kernel.  Short requests have a workgroup per item
+// instead, which needs neither the plan nor the join (attend_direct has the rule and the figures).
 //
 // The mathematics of a piece, per query row: a shift m, l = sum 2^(x_t - m) and o = sum 2^(x_t - m) v_t
 // over its entries, x_t = sm_scale log2(e) q.k_t.  Two pieces join as m = max(m1, m2),
@@ -28,7 +29,7 @@ static_assert(kStep == 2 * kPageSize, "a step is two pages");
 // gives the same sums to rounding while nothing overflows, and a rescaling costs a pass over o.
 constexpr float kLazy = 8.0f;
 constexpr float kNegInf = -__builtin_inff();
-constexpr int kItemCost = 6;
+constexpr int kItemCost = 6;         // see item_cost
 constexpr float kLn2 = 0.6931471805599453f;
 
 // Waves of a workgroup, which has a CU to itself: two on every SIMD, or one where the rows' registers
@@ -525,7 +526,7 @@ void attend_kernel(AttendArgs a) {
         }
       };
       if (kw == 1) {
-        // the wave's rows are the piece's: lane2 l holds elements 2 kE c' .. of row i
+        // the wave's rows are the piece's: register v of lane 16 c + i holds elements kE (4 c + v) .. of row i
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
           const float l = xor_sum(xor_sum(st.l[rt], 16), 32);

@@ -5,9 +5,9 @@
 // release reads the entries.  Both are bound by their atomics on the counts (25 a nanosecond over the
 // card), so one is made for several entries: the forks of a parent that follow each other count its
 // pages once, and a release takes off at once what a column of its list names in a run, as the
-// branches' rows of one parent do (branch_batch: fork 24 -> 10.5 us, counts of the release 22 -> 7.5).  The pages a release frees are
-// listed by page id through a bitmap of the pool, so the list does not depend on the order in which
-// the counts' atomics land.
+// branches' rows of one parent do (32 x 8 branches of 30,000-35,000 entries: fork 24 -> 10.5 us, counts of the
+// release 22 -> 7.5).  The pages a release frees are listed by page id through a bitmap of the pool, so
+// the list does not depend on the order in which the counts' atomics land.
 #include "device_common.hpp"
 
 namespace actkv {
@@ -180,7 +180,8 @@ __global__ __launch_bounds__(kReleaseSmall) void release_small_kernel(const int3
   __syncthreads();
   if (tid < n) {
     const int32_t page = pages[tid];
-    if (in_pool(page, num_pages) && came_to_zero(refs + page, atomicSub(refs + page, 1), 1)) gone[atomicAdd(&count, 1)] = page;
+    if (in_pool(page, num_pages) && came_to_zero(refs + page, atomicSub(refs + page, 1), 1))
+      gone[atomicAdd(&count, 1)] = page;
   }
   __syncthreads();
   const int total = count;

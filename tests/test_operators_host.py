@@ -60,6 +60,13 @@ def test_attend_refuses_problems(over, code):
     assert attend_bytes(p)[0] == code and c_attend(p) == code
 
 
+def test_attend_refuses_requests_past_the_entry_numbers():
+    for length, code in ((1 << 30, 0), ((1 << 30) + 1, UNSUPPORTED), ((1 << 31) - 1, UNSUPPORTED)):
+        p = problem(seq_lens=[length], q_lens=[1], budgets=[0], num_kv_heads=1, bt_stride=1 << 27)
+        assert attend_bytes(p)[0] == code
+        assert c_attend(p, ws_bytes=64) == (code or SMALL)
+
+
 def test_attend_workspace_is_the_limit():
     code, need = attend_bytes(problem())
     assert code == 0 and need > 0
