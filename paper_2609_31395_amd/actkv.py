@@ -865,8 +865,11 @@ class _Launch:
             torch.cuda.set_device(self._before)
 
     def _torch_stream(self):
-        return (self.given if isinstance(self.given, torch.cuda.Stream)
-                else torch.cuda.ExternalStream(self.handle, device=self.like.device))
+        if isinstance(self.given, torch.cuda.Stream):
+            return self.given
+        if not self.handle:   # (ExternalStream takes a null handle for none and gives a side stream)
+            return torch.cuda.default_stream(self.like.device)
+        return torch.cuda.ExternalStream(self.handle, device=self.like.device)
 
     def scratch(self, size: int) -> torch.Tensor:
         if self.given is None:
