@@ -562,7 +562,8 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
  * that hold +inf or NaN have unspecified values (never a fault; top_tokens stay within [-1, vocab)).
  * Sums are fp32 per chunk of the row in a fixed order, joined in fp64: results do not depend on
  * scheduling.  top_k in 0..64, vocab up to 262,144, rows up to 2^20 (else ACTKV_ERR_UNSUPPORTED).
- * workspace: at least the bytes that actkv_token_logprobs_workspace reports.
+ * workspace: at least the bytes that actkv_token_logprobs_workspace reports; so many serve every call
+ * of no more rows, vocab and top_k.
  */
 typedef enum actkv_logits_type {
   ACTKV_LOGITS_F32 = 0,

@@ -361,9 +361,16 @@ hipError_t launch_release(const int32_t* pages, int64_t n, int64_t row_len, int6
                           int32_t* refs, int32_t* freed, int32_t* num_freed, uint32_t* bits,
                           uint32_t* counts, hipStream_t s);
 // Token log probabilities: logprobs_splits chunks to a row (at most 64); stats holds 3 floats and top
-// k keys per chunk.
+// k keys per chunk.  Small chunks while the large ones of all rows are fewer than kLogprobsFew and a
+// row's candidates at most kLogprobsCand.
 constexpr int kLogprobsChunk = 16384, kLogprobsSmallChunk = 4096;
-int logprobs_splits(int64_t rows, int64_t vocab, int k);
+constexpr int kLogprobsFew = 512, kLogprobsCand = 1024;
+inline int64_t logprobs_large(int64_t vocab) { return (vocab + kLogprobsChunk - 1) / kLogprobsChunk; }
+inline int64_t logprobs_small(int64_t vocab) { return (vocab + kLogprobsSmallChunk - 1) / kLogprobsSmallChunk; }
+inline int logprobs_splits(int64_t rows, int64_t vocab, int k) {
+  const int64_t large = logprobs_large(vocab), small = logprobs_small(vocab);
+  return (int)(rows * large < kLogprobsFew && small * k <= kLogprobsCand ? small : large);
+}
 hipError_t launch_token_logprobs(const void* logits, int type, int64_t rows, int64_t vocab,
                                  int64_t row_stride, const int64_t* tokens, int k, float* logprobs,
                                  float* entropy, int64_t* top_tokens, float* top_logprobs,

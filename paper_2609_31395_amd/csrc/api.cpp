@@ -3,6 +3,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 #include <new>
@@ -1100,14 +1101,21 @@ actkv_status check_logprobs(int64_t rows, int64_t vocab, int32_t top_k) {
   return ACTKV_OK;
 }
 size_t logprobs_stats(int64_t chunks) { return actkv::align256(3 * sizeof(float) * (size_t)chunks); }
+size_t logprobs_bytes(int64_t chunks, int64_t keys) { return logprobs_stats(chunks) + sizeof(uint64_t) * (size_t)keys; }
 }  // namespace
 
 actkv_status actkv_token_logprobs_workspace(int64_t rows, int64_t vocab, int32_t top_k,
                                             size_t* workspace_bytes) {
   const actkv_status st = check_logprobs(rows, vocab, top_k);
   if (st != ACTKV_OK) return st;
-  const int64_t chunks = rows * actkv::logprobs_splits(rows, vocab, top_k);
-  if (workspace_bytes) *workspace_bytes = logprobs_stats(chunks) + sizeof(uint64_t) * (size_t)(chunks * top_k);
+  if (!workspace_bytes) return ACTKV_OK;
+  // What any call of no more rows, vocab and top_k takes: in large chunks, or, with its large ones fewer
+  // than kLogprobsFew and so at most four times as many small ones, in those.
+  const int64_t large = rows * actkv::logprobs_large(vocab), small = actkv::logprobs_small(vocab);
+  const int64_t most = 4 * (actkv::kLogprobsFew - 1);
+  const int64_t row_keys = std::min<int64_t>(small * top_k, actkv::kLogprobsCand);
+  *workspace_bytes = std::max(logprobs_bytes(large, large * top_k),
+                              logprobs_bytes(std::min(rows * small, most), std::min(rows * row_keys, most * top_k)));
   return ACTKV_OK;
 }
 
@@ -1117,8 +1125,7 @@ actkv_status actkv_token_logprobs(const void* logits, int32_t logits_type, int64
                                   int64_t* top_tokens, float* top_logprobs, void* workspace,
                                   size_t workspace_bytes, void* stream) {
   if (!top_tokens && !top_logprobs) top_k = 0;
-  size_t need = 0;
-  const actkv_status st = actkv_token_logprobs_workspace(rows, vocab, top_k, &need);
+  const actkv_status st = check_logprobs(rows, vocab, top_k);
   if (st != ACTKV_OK) return st;
   if (logits_type < ACTKV_LOGITS_F32 || logits_type > ACTKV_LOGITS_F16 || row_stride < vocab)
     return ACTKV_ERR_INVALID_ARGUMENT;
@@ -1127,14 +1134,14 @@ actkv_status actkv_token_logprobs(const void* logits, int32_t logits_type, int64
   if (!logits || reinterpret_cast<uintptr_t>(logits) % size) return ACTKV_ERR_INVALID_ARGUMENT;
   if (logprobs && !tokens) return ACTKV_ERR_INVALID_ARGUMENT;
   if (top_k > 0 && (!top_tokens || !top_logprobs)) return ACTKV_ERR_INVALID_ARGUMENT;
-  if (workspace_bytes < need) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
+  const int64_t chunks = rows * actkv::logprobs_splits(rows, vocab, top_k);
+  if (workspace_bytes < logprobs_bytes(chunks, chunks * top_k)) return ACTKV_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7)) return ACTKV_ERR_INVALID_ARGUMENT;
   char* base = static_cast<char*>(workspace);
   return hip_status(actkv::launch_token_logprobs(
       logits, logits_type, rows, vocab, row_stride, tokens, top_k, logprobs, entropy, top_tokens,
       top_logprobs, reinterpret_cast<float*>(base),
-      reinterpret_cast<unsigned long long*>(base + logprobs_stats(rows * actkv::logprobs_splits(rows, vocab, top_k))),
-      static_cast<hipStream_t>(stream)));
+      reinterpret_cast<unsigned long long*>(base + logprobs_stats(chunks)), static_cast<hipStream_t>(stream)));
 }
 
 const char* actkv_status_str(actkv_status status) {

@@ -20,7 +20,7 @@ namespace actkv {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kCand = 1024;               // candidates ranked in LDS, of a chunk or of a row
+constexpr int kCand = kLogprobsCand;      // candidates ranked in LDS, of a chunk or of a row
 
 typedef unsigned long long u64;
 
@@ -339,18 +339,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_row_kernel(
   }
 }
 
-int logprobs_splits(int64_t rows, int64_t vocab, int k) {
-  const int64_t large = (vocab + kLogprobsChunk - 1) / kLogprobsChunk;
-  const int64_t small = (vocab + kLogprobsSmallChunk - 1) / kLogprobsSmallChunk;
-  return (int)(rows * large < 512 && small * k <= kCand ? small : large);
-}
-
 hipError_t launch_token_logprobs(const void* logits, int type, int64_t rows, int64_t vocab,
                                  int64_t row_stride, const int64_t* tokens, int k, float* logprobs,
                                  float* entropy, int64_t* top_tokens, float* top_logprobs,
                                  float* stats, unsigned long long* top, hipStream_t s) {
   const int splits = logprobs_splits(rows, vocab, k);
-  const bool small = splits > (vocab + kLogprobsChunk - 1) / kLogprobsChunk;
+  const bool small = splits > logprobs_large(vocab);
   auto run = [&](auto zero) {
     using T = decltype(zero);
     const T* x = static_cast<const T*>(logits);
