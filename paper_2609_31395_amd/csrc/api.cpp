@@ -911,6 +911,23 @@ struct AttendPlan {
   size_t start = 0, q_off = 0, part_ml = 0, part_o = 0, total = 0;
 };
 
+// Partials of a call with `head_waves` heads side by side: two per workgroup and head of it.
+int64_t attend_slots(const AttendPlan& ap, int head_waves) {
+  const int64_t slots = (int64_t)actkv::kAttendMaxWgs * head_waves, steps = ap.steps * ap.hp.Hkv;
+  return 2 * (slots < steps ? slots : steps);
+}
+
+// Lays the workspace out for partials of so many rows.
+void carve_attend(AttendPlan* ap, int64_t part_rows) {
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = actkv::align256(o + bytes); return at; };
+  ap->start = take(sizeof(int32_t) * (size_t)((int64_t)ap->hp.R * ap->hp.Hkv + 1));
+  ap->q_off = take(sizeof(int32_t) * (size_t)ap->hp.R);
+  ap->part_ml = take(2 * sizeof(float) * (size_t)part_rows);
+  ap->part_o = take(sizeof(float) * (size_t)(part_rows * ap->hp.D));
+  ap->total = o;
+}
+
 actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   const actkv_status st = plan_host(p, &ap->hp);
   if (st != ACTKV_OK) return st;
@@ -924,17 +941,8 @@ actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
   const int64_t segs = (int64_t)hp.R * hp.Hkv;
   // (2^22 segments: a grid's threads stay below 2^32)
   if (ap->steps * hp.Hkv > INT32_MAX / 4 || segs > (1 << 22)) return ACTKV_ERR_UNSUPPORTED;
-  // two partials per workgroup and head of it
   ap->head_waves = actkv::attend_head_waves(hp.Hkv, hp.D, ap->max_rows, hp.sum_L);
-  int64_t slots = (int64_t)actkv::kAttendMaxWgs * ap->head_waves;
-  slots = 2 * (slots < ap->steps * hp.Hkv ? slots : ap->steps * hp.Hkv);
-  size_t o = 0;
-  auto take = [&](size_t bytes) { const size_t at = o; o = actkv::align256(o + bytes); return at; };
-  ap->start = take(sizeof(int32_t) * (size_t)(segs + 1));
-  ap->q_off = take(sizeof(int32_t) * (size_t)hp.R);
-  ap->part_ml = take(2 * sizeof(float) * (size_t)(slots * ap->max_rows));
-  ap->part_o = take(sizeof(float) * (size_t)(slots * ap->max_rows * hp.D));
-  ap->total = o;
+  carve_attend(ap, attend_slots(*ap, ap->head_waves) * ap->max_rows);
   return ACTKV_OK;
 }
 
@@ -944,6 +952,13 @@ actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_by
   AttendPlan ap;
   const actkv_status st = plan_attend(p, &ap);
   if (st != ACTKV_OK) return st;
+  // what any call of fewer rows takes too: it may have more heads side by side, and so more partials
+  int64_t rows = 0;
+  for (int64_t m = 1; m <= ap.max_rows; ++m) {
+    const int64_t r = m * attend_slots(ap, actkv::attend_head_waves(ap.hp.Hkv, ap.hp.D, m, ap.hp.sum_L));
+    rows = r > rows ? r : rows;
+  }
+  carve_attend(&ap, rows);
   if (workspace_bytes) *workspace_bytes = ap.total;
   return ACTKV_OK;
 }
