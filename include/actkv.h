@@ -485,10 +485,10 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
  * ACTKV_ATTEND_MAX_ROWS query rows per KV head and request (n_r * G), 2^30 entries of a request, 2^22
  * (request, KV head) pairs and a new_stride of 2^26: ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte
  * aligned (lse and kv_lens: 4).  k_new, v_new, q, out and lse must not overlap the cache, nor out and
- * lse what the call reads.  budgets are not used.  workspace: at least the bytes that
- * actkv_attend_workspace reports (host only, callable without a device); so many serve every problem of
- * the same heads whose requests are no more and, one by one, have no more entries and tokens.  No
- * atomics: results do not depend on scheduling.
+ * lse what the call reads.  Of p, budgets, pool_window and agg are not looked at (budgets may be NULL).
+ * workspace: at least the bytes that actkv_attend_workspace reports (host only, callable without a
+ * device); so many serve every problem of the same heads whose requests are no more and, one by one,
+ * have no more entries and tokens.  No atomics: results do not depend on scheduling.
  */
 #define ACTKV_ATTEND_MAX_ROWS 64
 actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_bytes);

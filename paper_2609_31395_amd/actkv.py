@@ -132,12 +132,12 @@ class _Cache:
     compaction returns.  The struct holds the addresses of the host arrays `arrays`, which live as
     long as it does; `given` are the Problem's own, of which they may be copies."""
     __slots__ = ("key", "given", "arrays", "struct", "ref", "query", "sizes", "inplace_freed",
-                 "attend_ws")
+                 "attend_sizes")
 
     def __init__(self, key, given, arrays, struct):
         self.key, self.given, self.arrays = key, given, arrays
         self.struct, self.ref = struct, ctypes.byref(struct)
-        self.query = self.sizes = self.inplace_freed = self.attend_ws = None
+        self.query = self.sizes = self.inplace_freed = self.attend_sizes = None
 
 
 @dataclass
@@ -888,18 +888,28 @@ class _Launch:
         return t
 
 
-def _attend_ws(cache: _Cache) -> int:
-    if cache.attend_ws is None:
+def _attend_sizes(p: Problem) -> dict:
+    """Element counts of the arrays attend() takes and the bytes of its workspace; what only a
+    compression reads of p (its budgets among it) is not looked at."""
+    cache = p._cached()
+    if cache.attend_sizes is None:
+        R, N = p.num_reqs, int(p.q_lens.astype(np.int64).sum())
+        if p.q_lens.shape[0] != R:
+            raise ValueError(f"q_lens holds {p.q_lens.shape[0]} requests, seq_lens {R}")
         need = ctypes.c_size_t()
         _check("actkv_attend_workspace",
                load_library().actkv_attend_workspace(cache.ref, ctypes.byref(need)))
-        cache.attend_ws = need.value
-    return cache.attend_ws
+        cache.attend_sizes = dict(
+            ref=cache.ref, reqs=R, tokens=N, q=N * p.num_q_heads * p.head_dim,
+            lse=N * p.num_q_heads, lens=R * p.num_kv_heads, bt=R * int(p.bt_stride),
+            kv=2 * int(p.num_pages) * p.page_size * p.num_kv_heads * p.head_dim if p.seq_lens.any() else 0,
+            ws=need.value)
+    return cache.attend_sizes
 
 
 def attend_workspace(p: Problem, device="cuda") -> torch.Tensor:
-    """A workspace for attend() on p."""
-    return torch.empty(max(_attend_ws(p._cached()), 1), dtype=torch.uint8, device=device)
+    """A workspace for attend() on p, and on every problem of its heads that is no larger."""
+    return torch.empty(max(_attend_sizes(p)["ws"], 1), dtype=torch.uint8, device=device)
 
 
 def _token_rows(name: str, t, rows: int, heads: int, dim: int, seen: list) -> int:
@@ -930,34 +940,37 @@ def attend(p: Problem, q: torch.Tensor, kv_cache: torch.Tensor, block_table: tor
     to the cache first.  q, k_new and v_new may be parts of one fused projection (rows further
     apart).  Returns (out [sum n, Hq, D], lse [sum n, Hq])."""
     lib = load_library()
-    z = _Sizes(p)
+    z, seen = _attend_sizes(p), []
+    N = z["tokens"]
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new go together")
-    q_stride = _token_rows("q", q, z.sum_n, p.num_q_heads, p.head_dim, z.seen)
+    q_stride = _token_rows("q", q, N, p.num_q_heads, p.head_dim, seen)
     new_stride = 0
     if k_new is not None:
-        new_stride = _token_rows("k_new", k_new, z.sum_n, p.num_kv_heads, p.head_dim, z.seen)
-        if _token_rows("v_new", v_new, z.sum_n, p.num_kv_heads, p.head_dim, z.seen) != new_stride:
+        new_stride = _token_rows("k_new", k_new, N, p.num_kv_heads, p.head_dim, seen)
+        if _token_rows("v_new", v_new, N, p.num_kv_heads, p.head_dim, seen) != new_stride:
             raise ValueError("k_new and v_new must have the same distance between rows")
-    z.need("kv_cache", kv_cache, _BITS16, z.kv if z.scores else 0)
-    z.need("block_table", block_table, _I32, z.bt)
-    z.need("kv_lens", kv_lens, _I32, z.lens, required=False)
-    z.need("out", out, _BITS16, z.q, required=False)
-    z.need("lse", lse, _F32, z.lse, required=False)
-    need = _attend_ws(z.cache)
+    _arg(seen, "kv_cache", kv_cache, _BITS16, z["kv"])
+    _arg(seen, "block_table", block_table, _I32, z["bt"])
+    _arg(seen, "kv_lens", kv_lens, _I32, z["lens"], required=False)
+    _arg(seen, "out", out, _BITS16, z["q"], required=False)
+    _arg(seen, "lse", lse, _F32, z["lse"], required=False)
+    need = z["ws"]
     if ws is not None:
-        _need("ws", ws, None, 0, seen=z.seen)
+        _need("ws", ws, None, 0, seen=seen)
         if _ws_bytes(ws) < need:
             raise ValueError(f"ws holds {_ws_bytes(ws)} bytes, the call needs {need}")
-    _on_gpu(z.seen + z.mirrors)
+    _arg(seen, "seq_lens_d", p.seq_lens_d, _I32, z["reqs"])
+    _arg(seen, "q_lens_d", p.q_lens_d, _I32, z["reqs"])
+    _on_gpu(seen)
     with _Launch(q, stream) as on:
         if out is None:
-            out = on.result((z.sum_n, p.num_q_heads, p.head_dim), torch.bfloat16)
+            out = on.result((N, p.num_q_heads, p.head_dim), torch.bfloat16)
         if lse is None:
-            lse = on.result((z.sum_n, p.num_q_heads), torch.float32)
+            lse = on.result((N, p.num_q_heads), torch.float32)
         ws = on.scratch(need) if ws is None else ws
         _check("actkv_attend", lib.actkv_attend(
-            z.ref, _ptr(q), q_stride, _ptr(kv_cache), _ptr(block_table), _ptr(kv_lens), _ptr(k_new),
+            z["ref"], _ptr(q), q_stride, _ptr(kv_cache), _ptr(block_table), _ptr(kv_lens), _ptr(k_new),
             _ptr(v_new), new_stride, _ptr(out), _ptr(lse), _ptr(ws), _ws_bytes(ws), on.handle))
     return out, lse
 

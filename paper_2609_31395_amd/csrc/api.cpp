@@ -49,26 +49,28 @@ int64_t request_fresh_pages(const actkv_problem* p, int r) {
   return bmin < L ? (kmax + actkv::kPageSize - 1) / actkv::kPageSize : 0;
 }
 
-// Validates `p` and derives the host plan from the host mirrors.  Touches no device memory.
-actkv_status plan_host(const actkv_problem* p, HostPlan* hp) {
+// Validates `p` and derives the host plan from the host mirrors.  Touches no device memory.  Without
+// `evicts` what only a compression takes (budgets, pooling window, aggregation) is neither read nor
+// planned.
+actkv_status plan_host(const actkv_problem* p, HostPlan* hp, bool evicts = true) {
   if (!p) return ACTKV_ERR_INVALID_ARGUMENT;
   if (p->num_reqs < 0 || p->num_q_heads <= 0 || p->num_kv_heads <= 0 || p->head_dim <= 0 ||
       p->page_size <= 0 || p->num_pages <= 0 || p->bt_stride <= 0)
     return ACTKV_ERR_INVALID_ARGUMENT;
   if (p->num_q_heads % p->num_kv_heads) return ACTKV_ERR_INVALID_ARGUMENT;
-  if (!valid_pool_window(p->pool_window)) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (evicts && !valid_pool_window(p->pool_window)) return ACTKV_ERR_INVALID_ARGUMENT;
   if (p->causal != 0 && p->causal != 1) return ACTKV_ERR_INVALID_ARGUMENT;
-  if (p->agg != ACTKV_AGG_SUM && p->agg != ACTKV_AGG_MAX_MEAN) return ACTKV_ERR_INVALID_ARGUMENT;
+  if (evicts && p->agg != ACTKV_AGG_SUM && p->agg != ACTKV_AGG_MAX_MEAN) return ACTKV_ERR_INVALID_ARGUMENT;
   if (!isfinite(p->sm_scale) || p->sm_scale < 0.f) return ACTKV_ERR_INVALID_ARGUMENT;
   if (p->flags & ~(ACTKV_FLAG_PLANNED | ACTKV_FLAG_SMALL_SELECT)) return ACTKV_ERR_INVALID_ARGUMENT;
   if (p->head_dim != 64 && p->head_dim != 128) return ACTKV_ERR_UNSUPPORTED;
   if (p->page_size != actkv::kPageSize) return ACTKV_ERR_UNSUPPORTED;
   if (p->num_kv_heads > 64) return ACTKV_ERR_UNSUPPORTED;
   const int32_t G = p->num_q_heads / p->num_kv_heads;
-  if (p->agg == ACTKV_AGG_MAX_MEAN && !(G == 1 || G == 2 || G == 4 || G == 8 || G == 16))
+  if (evicts && p->agg == ACTKV_AGG_MAX_MEAN && !(G == 1 || G == 2 || G == 4 || G == 8 || G == 16))
     return ACTKV_ERR_UNSUPPORTED;
   if (p->num_reqs > 0) {
-    if (!p->seq_lens_h || !p->q_lens_h || !p->budgets_h) return ACTKV_ERR_INVALID_ARGUMENT;
+    if (!p->seq_lens_h || !p->q_lens_h || (evicts && !p->budgets_h)) return ACTKV_ERR_INVALID_ARGUMENT;
   }
   hp->R = p->num_reqs;
   hp->Hq = p->num_q_heads;
@@ -92,7 +94,7 @@ actkv_status plan_host(const actkv_problem* p, HostPlan* hp) {
   for (int r = 0; r < p->num_reqs; ++r) {
     const int64_t L = p->seq_lens_h[r], n = p->q_lens_h[r];
     int64_t kmax = 0, bmin = INT64_MAX;
-    for (int h = 0; h < p->num_kv_heads; ++h) {
+    for (int h = 0; evicts && h < p->num_kv_heads; ++h) {
       const int64_t b = p->budgets_h[(int64_t)r * p->num_kv_heads + h];
       if (b < 0) return ACTKV_ERR_INVALID_ARGUMENT;
       const int64_t k = b < L ? b : L;
@@ -929,7 +931,7 @@ void carve_attend(AttendPlan* ap, int64_t part_rows) {
 }
 
 actkv_status plan_attend(const actkv_problem* p, AttendPlan* ap) {
-  const actkv_status st = plan_host(p, &ap->hp);
+  const actkv_status st = plan_host(p, &ap->hp, false);
   if (st != ACTKV_OK) return st;
   const HostPlan& hp = ap->hp;
   ap->max_rows = hp.max_n * hp.G;
