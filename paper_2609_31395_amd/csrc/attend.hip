@@ -475,7 +475,8 @@ void attend_kernel(AttendArgs a) {
       const int tid2 = opaque(tid), lane2 = tid2 & 63, c2 = lane2 >> 4, i2 = lane2 & 15;
       // the pieces of a head's key waves joined, 16 rows at a time
       auto join_waves = [&](auto key_waves) {
-        constexpr int kW = decltype(key_waves)::value, kH = kWaves / kW > 0 ? kWaves / kW : 1;
+        constexpr int kW = decltype(key_waves)::value, kH = kWaves / kW;
+        static_assert(kW * kH == kWaves, "the waves of a workgroup, by keys and heads");
 #pragma unroll
         for (int rt = 0; rt < kRowTiles; ++rt) {
           const float l = xor_sum(xor_sum(st.l[rt], 16), 32);
@@ -542,10 +543,11 @@ void attend_kernel(AttendArgs a) {
         }
       } else if (kw == 2) {
         join_waves(std::integral_constant<int, 2>());
-      } else if (kw == 4) {
-        join_waves(std::integral_constant<int, 4>());
+      } else if constexpr (kWaves == 8) {
+        if (kw == 4) join_waves(std::integral_constant<int, 4>());
+        else join_waves(std::integral_constant<int, 8>());
       } else {
-        join_waves(std::integral_constant<int, 8>());
+        join_waves(std::integral_constant<int, 4>());
       }
     }
     start += cost_of(it);
