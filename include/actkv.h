@@ -536,7 +536,8 @@ actkv_status actkv_release_pages(const int32_t* pages, int64_t n, int64_t row_le
  * live requests is counted).  forks_h: host array of num_forks, forks_d its device mirror.  Rows lie
  * in [0, num_rows); a child is nobody's parent and the child of one fork only, and pages <=
  * bt_stride (at most 2^23; at most 65,535 forks).  free_pages lists each page once and no live one;
- * fewer than needed: ACTKV_ERR_OUT_OF_PAGES.  What a child's row held is overwritten (release it first).
+ * fewer than needed: ACTKV_ERR_OUT_OF_PAGES; more than 2^31 - 1 needed: ACTKV_ERR_UNSUPPORTED.  What a
+ * child's row held is overwritten (release it first).
  */
 typedef struct actkv_fork {
   int32_t parent, child, shared, pages;

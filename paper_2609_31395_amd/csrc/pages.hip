@@ -23,22 +23,36 @@ __device__ __forceinline__ bool in_pool(int64_t page, int64_t num_pages) {
 
 }  // namespace
 
-// Grid: (row workgroups + the most pages one fork copies, forks).  The first write kRowEntries of the
-// child's row and count the shared pages; each of the others copies a page, K and V.
+// Workgroups: row_wgs for the row of each fork, then one for each page that is copied (`fresh` of them over
+// all forks, numbered as the fresh pages are).  The first write kRowEntries of the child's row and count the
+// shared pages; each of the others finds its fork and copies a page, K and V.
 __global__ __launch_bounds__(kThreads) void fork_kernel(
-    const actkv_fork* forks, int num_forks, int row_wgs, int32_t bt_stride, int64_t num_pages, int64_t page_vecs,
-    u32x4* kv, int32_t* bt, const int32_t* free_pages, int32_t* refs) {
+    const actkv_fork* forks, int num_forks, int row_wgs, uint32_t fresh, int32_t bt_stride, int64_t num_pages,
+    int64_t page_vecs, u32x4* kv, int32_t* bt, const int32_t* free_pages, int32_t* refs) {
   __shared__ int64_t scan_s[17];
-  const int f = blockIdx.y, tid = threadIdx.x;
-  const actkv_fork fk = forks[f];
-  int64_t mine = 0, off;   // off: fresh pages of the forks before
-  for (int x = tid; x < f; x += kThreads) mine += forks[x].pages - forks[x].shared;
-  block_excl_scan_i64(mine, scan_s, &off);
-  const int32_t* parent = bt + (int64_t)fk.parent * bt_stride;
-  if ((int)blockIdx.x >= row_wgs) {
-    const int x = (int)blockIdx.x - row_wgs;
-    if (x >= fk.pages - fk.shared) return;
-    const int64_t src = parent[fk.shared + x], dst = free_pages[off + x];
+  const int tid = threadIdx.x;
+  const uint32_t rows = (uint32_t)num_forks * (uint32_t)row_wgs, wg = blockIdx.y * gridDim.x + blockIdx.x;
+  if (wg >= rows) {
+    const uint32_t x = wg - rows;
+    if (x >= fresh) return;
+    __shared__ int64_t parent_s;   // where the page's parent is entered
+    const int64_t dst = free_pages[x];
+    const int per = (num_forks + kThreads - 1) / kThreads, f0 = tid * per, f1 = min(f0 + per, num_forks);
+    int64_t mine = 0, all;
+    for (int f = f0; f < f1; ++f) mine += forks[f].pages - forks[f].shared;
+    int64_t before = block_excl_scan_i64(mine, scan_s, &all);
+    if ((int64_t)x >= all) return;
+    if (before <= x && x < before + mine)
+      for (int f = f0; f < f1; ++f) {
+        const actkv_fork fk = forks[f];
+        const int64_t i = x - before;
+        before += fk.pages - fk.shared;
+        if (x >= before) continue;
+        parent_s = (int64_t)fk.parent * bt_stride + fk.shared + i;
+        break;
+      }
+    __syncthreads();
+    const int64_t src = bt[parent_s];
     if (!in_pool(src, num_pages) || !in_pool(dst, num_pages)) return;
     for (int64_t i = tid; i < page_vecs; i += kThreads) {
       kv[dst * page_vecs + i] = kv[src * page_vecs + i];
@@ -46,6 +60,12 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(
     }
     return;
   }
+  const int f = (int)(wg / (uint32_t)row_wgs), row_wg = (int)(wg - (uint32_t)f * row_wgs);
+  const actkv_fork fk = forks[f];
+  int64_t mine = 0, off;   // off: fresh pages of the forks before
+  for (int x = tid; x < f; x += kThreads) mine += forks[x].pages - forks[x].shared;
+  block_excl_scan_i64(mine, scan_s, &off);
+  const int32_t* parent = bt + (int64_t)fk.parent * bt_stride;
   // the shared pages of the forks of this parent in this fork's group of 64: a run of them counts a
   // page once
   __shared__ int32_t shared_s[64];
@@ -58,13 +78,13 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(
   int32_t page[kPer];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const int i = blockIdx.x * kRowEntries + k * kThreads + tid;
+    const int i = row_wg * kRowEntries + k * kThreads + tid;
     page[k] = i < fk.shared ? parent[i] : i < fk.pages ? free_pages[off + i - fk.shared] : -1;
   }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    const int i = blockIdx.x * kRowEntries + k * kThreads + tid;
+    const int i = row_wg * kRowEntries + k * kThreads + tid;
     if (i >= bt_stride) continue;
     child[i] = page[k];
     if (!refs || !in_pool(page[k], num_pages)) continue;
@@ -204,12 +224,14 @@ unsigned blocks_for(int64_t n) {
 }
 }  // namespace
 
-hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t max_copied, int32_t bt_stride,
+hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t fresh, int32_t bt_stride,
                        int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
                        const int32_t* free_pages, int32_t* refs, hipStream_t s) {
   const int row_wgs = (bt_stride + kRowEntries - 1) / kRowEntries;
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)(row_wgs + max_copied), (unsigned)num_forks),
-                     dim3(kThreads), 0, s, forks, num_forks, row_wgs, bt_stride, num_pages, page_bytes / 16,
+  // (at most 2^29 for the rows and 2^31 for the pages: numbered in 32 bits, in rows of at most 2^20)
+  const int64_t wgs = (int64_t)num_forks * row_wgs + fresh, wide = wgs < (1 << 20) ? wgs : 1 << 20;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)wide, (unsigned)((wgs + wide - 1) / wide)), dim3(kThreads), 0, s,
+                     forks, num_forks, row_wgs, (uint32_t)fresh, bt_stride, num_pages, page_bytes / 16,
                      static_cast<u32x4*>(kv), bt, free_pages, refs);
   return hipGetLastError();
 }
