@@ -999,7 +999,8 @@ class Forks:
     def of_lengths(cls, parents, children, kv_lens, share: bool = True) -> "Forks":
         """kv_lens: entries of each (parent, KV head), [forks, Hkv] on the host.  Pages that are full
         in every head are shared, the others copied (with share False all of them)."""
-        lens = np.asarray(kv_lens).reshape(len(np.asarray(parents).reshape(-1)), -1)
+        n, lens = np.asarray(parents).size, np.asarray(kv_lens)
+        lens = lens.reshape(n, -1) if n > 0 or lens.size > 0 else np.zeros((0, 1), np.int32)
         return cls(parents, children, lens.min(axis=1) // PAGE_SIZE * int(bool(share)),
                    -(-lens.max(axis=1) // PAGE_SIZE))
 

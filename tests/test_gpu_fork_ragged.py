@@ -52,3 +52,13 @@ def test_parents_that_alternate(n):
         shared = int(rng.choice([0, 5, 1024, 1025, stride]))
         forks.append([parent(i), 3 + i, shared, min(stride, shared + int(rng.integers(0, 3)))])
     run(forks, 3, stride, 3 * stride + 3 * n, 3 + n, n)
+
+
+def test_no_fork_changes_nothing():
+    kv = torch.zeros(2, 6, 16, 1, 64, dtype=torch.int16, device=DEV)
+    bt = torch.full((3, 2), 5, dtype=torch.int32, device=DEV)
+    refs = torch.ones(6, dtype=torch.int32, device=DEV)
+    f = actkv.Forks.of_lengths([], [], np.zeros((0, 1)))
+    actkv.fork_pages(f, kv, bt, None, refs)
+    actkv.fork_pages(f.to_device(DEV), kv, bt, None, refs)
+    assert (bt == 5).all() and (refs == 1).all() and (kv == 0).all()
