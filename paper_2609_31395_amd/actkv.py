@@ -986,14 +986,21 @@ class Forks:
     device: Optional[torch.Tensor] = None
 
     def __post_init__(self):
-        cols = [np.asarray(c, dtype=np.int32).reshape(-1)
-                for c in (self.parents, self.children, self.shared, self.pages)]
+        cols = [self._column(name) for name in ("parents", "children", "shared", "pages")]
         if len({c.shape[0] for c in cols}) != 1:
             raise ValueError("parents, children, shared and pages must have the same length")
         self.host = np.ascontiguousarray(np.stack(cols, axis=1))
         self.host.setflags(write=False)   # the device mirror holds the same values
         self.parents, self.children, self.shared, self.pages = self.host.T
         self.num_fresh = int((self.pages.astype(np.int64) - self.shared).sum())
+
+    def _column(self, name: str) -> np.ndarray:
+        given = np.asarray(getattr(self, name)).reshape(-1)
+        with np.errstate(invalid="ignore"):
+            col = given.astype(np.int32)
+        if not np.array_equal(col, given):   # a row that the conversion would make up
+            raise ValueError(f"{name} must be whole numbers of 32 bits")
+        return col
 
     @classmethod
     def of_lengths(cls, parents, children, kv_lens, share: bool = True) -> "Forks":
