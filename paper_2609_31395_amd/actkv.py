@@ -849,6 +849,8 @@ class _Launch:
 
     def __enter__(self):
         index = self.like.get_device()
+        if getattr(self.given, "device_index", index) != index:
+            raise ValueError(f"stream is of cuda:{self.given.device_index}, the tensors on cuda:{index}")
         self._before = -1
         if torch._C._cuda_getDevice() != index:
             self._before = torch._C._cuda_getDevice()

@@ -47,3 +47,11 @@ def test_memory_is_made_for_the_stream_of_the_call(streams, handle, raw):
         on.scratch(64)
         on.result((3,), torch.float32)
     assert streams == [handle, handle]
+
+
+@pytest.mark.parametrize("device", [0, 3])
+def test_a_stream_of_another_device_is_refused(streams, device):
+    with pytest.raises(ValueError, match="stream"):   # a host tensor's device is -1
+        with actkv._Launch(torch.zeros(4), FakeStream(0x5000, device)):
+            pass
+    assert streams == []
