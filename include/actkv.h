@@ -463,8 +463,9 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
  * Decode attention over the paged cache (Sec. 2.3, Sec. 2.5): for every action query j < n_r of
  * request r -- here the request's newest tokens -- and query head g of KV head h,
  *   out = sum_t p_t v_t,  p_t = exp(sm_scale q . k_t - LSE),  LSE = log sum_t exp(sm_scale q . k_t)
- * over the entries t of (r, h) that it sees, and the LSE itself, which the scoring takes (Sec. 7.1:
- * a by-product of decode attention).
+ * over the entries t of (r, h) that it sees, and the LSE itself (Sec. 7.1: a by-product of decode
+ * attention).  The scoring takes that LSE where every head of a request has seq_lens[r] entries: it
+ * knows no lengths per head, and an LSE over fewer entries is not that of the ones it scores.
  *   kv_lens  device int32 [R * Hkv], or NULL for seq_lens[r] in every head: the entries of each
  *            (request, KV head), the newest tokens included, as a compaction with unequal budgets
  *            leaves them (new_lens, and n_r for the tokens appended since).  Read on the device, so
@@ -479,16 +480,18 @@ actkv_status actkv_check_pages(const actkv_problem* p, const int32_t* block_tabl
  *            parts of one fused projection have a larger stride).  Both strides: multiples of 8.
  *   out      bf16 [sum n][Hq][D]; lse (nullable) fp32 [sum n][Hq], natural log.
  * A query that sees no entry gets out = 0 and lse = -inf.  Slots past an entry count are never part
- * of the result, whatever they hold.  Entries behind a page outside [0, num_pages) have K and V of
- * zero (their logit is 0).  q, K and V of the entries are finite.  Sums and the softmax are fp32; the
- * probabilities enter the second product as the sum of two bf16 values (16 bits).  At most
- * ACTKV_ATTEND_MAX_ROWS query rows per KV head and request (n_r * G), 2^30 entries of a request, 2^22
- * (request, KV head) pairs and a new_stride of 2^26: ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte
- * aligned (lse and kv_lens: 4).  k_new, v_new, q, out and lse must not overlap the cache, nor out and
- * lse what the call reads.  Of p, budgets, pool_window and agg are not looked at (budgets may be NULL).
- * workspace: at least the bytes that actkv_attend_workspace reports (host only, callable without a
- * device); so many serve every problem of the same heads whose requests are no more and, one by one,
- * have no more entries and tokens.  No atomics: results do not depend on scheduling.
+ * of the result, whatever they hold.  Entries in the cache behind a page outside [0, num_pages) have
+ * K and V of zero (their logit is 0).  q, K and V of the entries are finite, the logits too in fp32,
+ * and V is below 2^88 in magnitude (weights reach 2^8 before the division, over up to 2^30 entries).
+ * Sums and the softmax are fp32; the probabilities enter the second product as the sum of two bf16
+ * values (16 bits).  At most ACTKV_ATTEND_MAX_ROWS query rows per KV head and request (n_r * G),
+ * 2^30 entries of a request, 2^22 (request, KV head) pairs and a new_stride of 2^26:
+ * ACTKV_ERR_UNSUPPORTED beyond.  Pointers 16-byte aligned (lse and kv_lens: 4).  k_new, v_new, q,
+ * out and lse must not overlap the cache, nor out and lse what the call reads.  Of p, budgets,
+ * pool_window and agg are not looked at (budgets may be NULL).  workspace: at least the bytes that
+ * actkv_attend_workspace reports (host only, callable without a device); so many serve every problem
+ * of the same heads whose requests are no more and, one by one, have no more entries and tokens.  No
+ * atomics: results do not depend on scheduling.
  */
 #define ACTKV_ATTEND_MAX_ROWS 64
 actkv_status actkv_attend_workspace(const actkv_problem* p, size_t* workspace_bytes);
