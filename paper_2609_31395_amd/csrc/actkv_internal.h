@@ -340,7 +340,7 @@ struct AttendArgs {
   const char* kv;
   uint16_t* out;
   float* lse;
-  int32_t* start;                       // workspace [R, with kv_lens R * Hkv, + 1]: steps before each item
+  int32_t* start;                       // workspace [R, with kv_lens R * Hkv, + 1]: cost before each item
   int32_t* q_off;                       // workspace [R]
   float* part_o;                        // workspace [2 * workgroups][Hkv_slots][max_rows][D]
   float2* part_ml;                      // workspace, the same without D: shift and sum

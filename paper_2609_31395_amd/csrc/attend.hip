@@ -32,9 +32,10 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr int kItemCost = 6;         // see item_cost
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Waves of a workgroup, which has a CU to itself: two on every SIMD, or one where the rows' registers
-// leave no room for two.  A wave has one step in flight; two or four of them, or two workgroups to a
-// CU, were no faster at any size (attend_batch the same; 64-element heads 78 against 73.5 us).
+// Waves of a workgroup: two on every SIMD, or one where the rows' registers leave no room for two.
+// With equal shares it has a CU to itself; with a workgroup per item several may share one or follow each
+// other.  A wave has one step in flight; two or four of them, or two workgroups to a CU, were no faster
+// with equal shares (attend_batch the same; 64-element heads 78 against 73.5 us).
 template <int D, int kRowTiles>
 struct Shape {
   static constexpr int kWaves = attend_waves(D, 16 * kRowTiles);

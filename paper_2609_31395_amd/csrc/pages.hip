@@ -6,7 +6,7 @@
 // card), so one is made for several entries: the forks of a parent that follow each other count its
 // pages once, and a release takes off at once what a column of its list names in a run, as the
 // branches' rows of one parent do (32 x 8 branches of 30,000-35,000 entries: fork 24 -> 10.5 us, counts of the
-// release 22 -> 7.5).  The pages a release frees are listed by page id through a bitmap of the pool, so
+// release 22 -> 7.5; the fork 8.9 with its workgroups numbered by rows and copied pages).  The pages a release frees are listed by page id through a bitmap of the pool, so
 // the list does not depend on the order in which the counts' atomics land.
 #include "device_common.hpp"
 
