@@ -352,8 +352,8 @@ constexpr int64_t kReleaseBlock = 8192;   // pages whose freed ones one workgrou
 constexpr int kReleaseRows = 8;           // rows of a list whose entries of a column one thread takes
 constexpr int kReleaseSmall = 1024;       // entries that one workgroup releases by itself
 inline int64_t release_blocks(int64_t num_pages) { return (num_pages + kReleaseBlock - 1) / kReleaseBlock; }
-hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t fresh, int32_t bt_stride,
-                       int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
+hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t fresh, int32_t max_copied,
+                       int32_t bt_stride, int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
                        const int32_t* free_pages, int32_t* refs, hipStream_t s);
 hipError_t launch_acquire(const int32_t* pages, int64_t n, int64_t num_pages, int32_t* refs,
                           hipStream_t s);

@@ -1084,6 +1084,7 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
   if (num_forks == 0) return ACTKV_OK;
   if (!forks_h || !forks_d || !block_table) return ACTKV_ERR_INVALID_ARGUMENT;
   int64_t fresh = 0;
+  int32_t most = 0;
   try {
     std::vector<uint8_t> row(num_rows, 0);   // 1: a parent, 2: a child
     for (int f = 0; f < num_forks; ++f) {
@@ -1095,6 +1096,7 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
       row[k.parent] = 1;
       row[k.child] = 2;
       fresh += k.pages - k.shared;
+      most = k.pages - k.shared > most ? k.pages - k.shared : most;
     }
   } catch (const std::bad_alloc&) {
     return ACTKV_ERR_HIP;
@@ -1104,7 +1106,7 @@ actkv_status actkv_fork_pages(const actkv_fork* forks_h, const actkv_fork* forks
   if (fresh > INT32_MAX) return ACTKV_ERR_UNSUPPORTED;   // more than there are page ids
   if (fresh > 0 && !free_pages) return ACTKV_ERR_INVALID_ARGUMENT;
   return hip_status(actkv::launch_fork(
-      forks_d, num_forks, fresh, bt_stride, num_pages,
+      forks_d, num_forks, fresh, most, bt_stride, num_pages,
       (int64_t)page_size * num_kv_heads * head_dim * 2, kv_cache, block_table, free_pages, refs,
       static_cast<hipStream_t>(stream)));
 }

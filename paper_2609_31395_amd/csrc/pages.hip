@@ -21,38 +21,97 @@ __device__ __forceinline__ bool in_pool(int64_t page, int64_t num_pages) {
   return page >= 0 && page < num_pages;
 }
 
-}  // namespace
+// The sum of v over the wave, in its last lane.  (32 bits: a fork has 2^23 pages at most.)
+__device__ __forceinline__ int32_t wave_last_sum(int32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return v;
+}
 
-// Workgroups: row_wgs for the row of each fork, then one for each page that is copied (`fresh` of them over
-// all forks, numbered as the fresh pages are).  The first write kRowEntries of the child's row and count the
-// shared pages; each of the others finds its fork and copies a page, K and V.
-__global__ __launch_bounds__(kThreads) void fork_kernel(
-    const actkv_fork* forks, int num_forks, int row_wgs, uint32_t fresh, int32_t bt_stride, int64_t num_pages,
-    int64_t page_vecs, u32x4* kv, int32_t* bt, const int32_t* free_pages, int32_t* refs) {
-  __shared__ int64_t scan_s[17];
-  const int tid = threadIdx.x;
-  const uint32_t rows = (uint32_t)num_forks * (uint32_t)row_wgs, wg = blockIdx.y * gridDim.x + blockIdx.x;
-  if (wg >= rows) {
-    const uint32_t x = wg - rows;
-    if (x >= fresh) return;
-    __shared__ int64_t parent_s;   // where the page's parent is entered
-    const int64_t dst = free_pages[x];
-    const int per = (num_forks + kThreads - 1) / kThreads, f0 = tid * per, f1 = min(f0 + per, num_forks);
-    int64_t mine = 0, all;
-    for (int f = f0; f < f1; ++f) mine += forks[f].pages - forks[f].shared;
-    int64_t before = block_excl_scan_i64(mine, scan_s, &all);
-    if ((int64_t)x >= all) return;
-    if (before <= x && x < before + mine)
-      for (int f = f0; f < f1; ++f) {
-        const actkv_fork fk = forks[f];
-        const int64_t i = x - before;
-        before += fk.pages - fk.shared;
-        if (x >= before) continue;
-        parent_s = (int64_t)fk.parent * bt_stride + fk.shared + i;
+// Where the parent of fresh page x is entered in the block table (-1: x is behind the last): the forks are
+// added up in chunks of 64, as many as a lane each can hold, until x lies in one of these, and every wave
+// then has a chunk's forks in its lanes.  For the whole workgroup; up to 64 forks take no barrier.
+constexpr int kForkChunks = 64;
+__device__ __forceinline__ int64_t parent_entry(const actkv_fork* forks, int num_forks, int64_t x, int32_t bt_stride,
+                                                int32_t* chunk_s) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  auto fresh_of = [&](int f) { return f < num_forks ? forks[f].pages - forks[f].shared : 0; };
+  // the lanes that x is behind, and what the pages of all of these come to
+  auto behind = [&](int64_t incl, int* lanes) {
+    *lanes = __popcll(__ballot(incl <= x));
+    return *lanes > 0 ? readlane_i64(incl, *lanes - 1) : 0;
+  };
+  int64_t before = 0;   // pages of the forks before `first`
+  int first = 0, k;
+  if (num_forks > 64)
+    for (;; first += 64 * kForkChunks) {
+      constexpr int kWaves = kThreads / 64, kPer = kForkChunks / kWaves;
+      int32_t n[kPer];   // a lane's forks of the wave's chunks, all loads in flight
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) n[c] = fresh_of(first + 64 * (kWaves * c + w) + lane);
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) {
+        n[c] = wave_last_sum(n[c]);
+        if (lane == 63) chunk_s[kWaves * c + w] = n[c];
+      }
+      __syncthreads();
+      const int64_t incl = before + wave_incl_scan_i64(chunk_s[lane]);
+      const int64_t all = readlane_i64(incl, 63);
+      if (x < all) {
+        const int64_t b = behind(incl, &k);
+        if (k > 0) before = b;
+        first += 64 * k;
         break;
       }
-    __syncthreads();
-    const int64_t src = bt[parent_s];
+      before = all;
+      if (first + 64 * kForkChunks >= num_forks) return -1;
+      __syncthreads();   // chunk_s is written again
+    }
+  const int64_t incl = before + wave_incl_scan_i64(fresh_of(first + lane));
+  const int64_t b = behind(incl, &k);
+  if (k == 64) return -1;
+  const actkv_fork fk = forks[first + k];
+  return (int64_t)fk.parent * bt_stride + fk.shared + (x - (k > 0 ? b : before));
+}
+
+}  // namespace
+
+// Workgroups: row_wgs for the row of each fork, which write kRowEntries of the child's row each and count
+// the shared pages; then, by `each`, that many for each fork, or (0) one for each page that is copied
+// (`fresh` of them, numbered as the fresh pages are), which copy a page, K and V.
+__global__ __launch_bounds__(kThreads) void fork_kernel(
+    const actkv_fork* forks, int num_forks, int row_wgs, int each, uint32_t fresh, int32_t bt_stride,
+    int64_t num_pages, int64_t page_vecs, u32x4* kv, int32_t* bt, const int32_t* free_pages, int32_t* refs) {
+  __shared__ int64_t scan_s[17];
+  __shared__ int32_t chunk_s[kForkChunks];
+  const int tid = threadIdx.x;
+  const uint32_t rows = (uint32_t)num_forks * (uint32_t)row_wgs, wg = blockIdx.y * gridDim.x + blockIdx.x;
+  // fresh pages of the forks before f
+  auto fresh_before = [&](int f) {
+    int64_t mine = 0, all;
+    for (int x = tid; x < f; x += kThreads) mine += forks[x].pages - forks[x].shared;
+    block_excl_scan_i64(mine, scan_s, &all);
+    return all;
+  };
+  if (wg >= rows) {
+    int64_t x = wg - rows, entry;
+    if (each > 0) {
+      const int f = (int)((uint32_t)x / (uint32_t)each), i = (int)((uint32_t)x - (uint32_t)f * each);
+      if (f >= num_forks) return;
+      const actkv_fork fk = forks[f];
+      if (i >= fk.pages - fk.shared) return;
+      x = fresh_before(f) + i;
+      entry = (int64_t)fk.parent * bt_stride + fk.shared + i;
+    } else {
+      if (x >= fresh) return;
+      entry = parent_entry(forks, num_forks, x, bt_stride, chunk_s);
+      if (entry < 0) return;
+    }
+    const int64_t src = bt[entry], dst = free_pages[x];
     if (!in_pool(src, num_pages) || !in_pool(dst, num_pages)) return;
     for (int64_t i = tid; i < page_vecs; i += kThreads) {
       kv[dst * page_vecs + i] = kv[src * page_vecs + i];
@@ -62,9 +121,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(
   }
   const int f = (int)(wg / (uint32_t)row_wgs), row_wg = (int)(wg - (uint32_t)f * row_wgs);
   const actkv_fork fk = forks[f];
-  int64_t mine = 0, off;   // off: fresh pages of the forks before
-  for (int x = tid; x < f; x += kThreads) mine += forks[x].pages - forks[x].shared;
-  block_excl_scan_i64(mine, scan_s, &off);
+  const int64_t off = fresh_before(f);
   const int32_t* parent = bt + (int64_t)fk.parent * bt_stride;
   // the shared pages of the forks of this parent in this fork's group of 64: a run of them counts a
   // page once
@@ -224,14 +281,20 @@ unsigned blocks_for(int64_t n) {
 }
 }  // namespace
 
-hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t fresh, int32_t bt_stride,
-                       int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
+hipError_t launch_fork(const actkv_fork* forks, int num_forks, int64_t fresh, int32_t max_copied,
+                       int32_t bt_stride, int64_t num_pages, int64_t page_bytes, void* kv, int32_t* bt,
                        const int32_t* free_pages, int32_t* refs, hipStream_t s) {
   const int row_wgs = (bt_stride + kRowEntries - 1) / kRowEntries;
+  // As many workgroups for each fork's copies while at most half of them are idle: a fork that is known
+  // needs no search (4,096 forks of 4 pages: 43 against 63 us, 16,384 of one 145 against 174; 256 of one 7.3
+  // and 7.4).  By page for unequal copies (256 forks of which one copies 2,188 pages: 2,956 workgroups in
+  // place of 560,896).
+  const int64_t even = (int64_t)num_forks * max_copied;
+  const int each = even <= 2 * fresh && even <= INT32_MAX ? max_copied : 0;
   // (at most 2^29 for the rows and 2^31 for the pages: numbered in 32 bits, in rows of at most 2^20)
-  const int64_t wgs = (int64_t)num_forks * row_wgs + fresh, wide = wgs < (1 << 20) ? wgs : 1 << 20;
+  const int64_t wgs = (int64_t)num_forks * row_wgs + (each > 0 ? even : fresh), wide = wgs < (1 << 20) ? wgs : 1 << 20;
   hipLaunchKernelGGL(fork_kernel, dim3((unsigned)wide, (unsigned)((wgs + wide - 1) / wide)), dim3(kThreads), 0, s,
-                     forks, num_forks, row_wgs, (uint32_t)fresh, bt_stride, num_pages, page_bytes / 16,
+                     forks, num_forks, row_wgs, each, (uint32_t)fresh, bt_stride, num_pages, page_bytes / 16,
                      static_cast<u32x4*>(kv), bt, free_pages, refs);
   return hipGetLastError();
 }

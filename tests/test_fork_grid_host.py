@@ -91,3 +91,13 @@ def test_fresh_pages_past_the_page_ids_are_refused(launches):
                    dict(forks=big[:255], rows=300, stride=1 << 23, free=1 << 40))
     assert [c for c, _ in got] == [-2, -4, 0]
     assert [len(g) for _, g in got] == [0, 0, 1]
+
+
+@pytest.mark.parametrize("n", [1, 2, 64, 1000, 5000])
+@pytest.mark.parametrize("most", [1, 3, 50])
+def test_at_most_half_of_the_copying_workgroups_are_idle(launches, n, most):
+    f = forks(n, lambda i: 60 - (i * 7919) % (most + 1), lambda i: 60)
+    fresh = sum(p - s for _, _, s, p in f)
+    [[code, grids]] = launches(dict(forks=f, rows=70000, stride=60, free=fresh))
+    assert code == 0 and len(grids) == 1
+    assert n + fresh <= grids[0][0] * grids[0][1] <= n + 2 * fresh + 64

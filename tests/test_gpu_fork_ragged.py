@@ -62,3 +62,13 @@ def test_no_fork_changes_nothing():
     actkv.fork_pages(f, kv, bt, None, refs)
     actkv.fork_pages(f.to_device(DEV), kv, bt, None, refs)
     assert (bt == 5).all() and (refs == 1).all() and (kv == 0).all()
+
+
+@pytest.mark.parametrize("n,copied_by", [(64, 64), (65, 65), (128, 1), (4096, 4096), (4097, 4097), (4160, 30), (8193, 8193),
+                                         (9000, 3)])
+def test_forks_past_what_is_added_up_at_a_time(n, copied_by):
+    """The last `copied_by` forks copy up to three pages each, the others none."""
+    rng = np.random.default_rng(n)
+    forks = [[int(rng.integers(0, 3)), 3 + i, 2, 2 if i < n - copied_by else 2 + int(rng.integers(0, 4))] for i in range(n)]
+    forks[-1][3] = 5   # the last page of all is the last fork's
+    run(forks, 3, 6, 18 + 3 * n, 3 + n, n)
