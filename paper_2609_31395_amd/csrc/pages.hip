@@ -2,12 +2,14 @@
 // actkv_release_pages) and forks of requests (actkv_fork_pages).
 //
 // A fork moves what it copies (a page is read and written once) and touches one table entry per page; a
-// release reads the entries.  Both are bound by their atomics on the counts (25 a nanosecond over the
-// card), so one is made for several entries: the forks of a parent that follow each other count its
-// pages once, and a release takes off at once what a column of its list names in a run, as the
-// branches' rows of one parent do (32 x 8 branches of 30,000-35,000 entries: fork 24 -> 10.5 us, counts of the
-// release 22 -> 7.5; the fork 8.9 with its workgroups numbered by rows and copied pages).  The pages a release frees are listed by page id through a bitmap of the pool, so
-// the list does not depend on the order in which the counts' atomics land.
+// release reads the entries.  An atomic on a count for each entry would bound both (25 a nanosecond over
+// the card), so one is made for several: the forks of a parent that follow each other count its pages
+// once, and a release takes off at once what a column of its list names in a run, as the branches' rows
+// of one parent do (32 x 8 branches of 30,000-35,000 entries, 560,000 of them: fork 24 -> 10.5 us, counts of
+// the release 22 -> 7.5; with the workgroups numbered by rows, then copies, the fork takes 8.7).  What is
+// left of these is 70,000 atomics each, 2.8 us, and chains of dependent loads.  The pages a release frees
+// are listed by page id through a bitmap of the pool, so the list does not depend on the order in which
+// the counts' atomics land.
 #include "device_common.hpp"
 
 namespace actkv {
